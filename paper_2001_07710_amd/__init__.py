@@ -14,9 +14,12 @@ from typing import Optional
 import numpy as np
 
 F32, F16 = 0, 1
+BF16 = 2                  # the entries of pconv_dense.h only
 FLAG_RELU = 1
 FLAG_DENSE_DIRECT = 2
 FLAG_NHWC = 4
+FLAG_RESIDUAL_FIRST = 8   # linear
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3, 4
 PACK_HOST_ONLY = 1
 KERNEL_AUTO, KERNEL_TILED, KERNEL_GENERIC, KERNEL_QUAD, KERNEL_MFMA = 0, 1, 2, 3, 4
 ORDER_AUTO, ORDER_PLAIN, ORDER_BALANCED = 0, 1, 2
@@ -110,6 +113,22 @@ def _load():
     lib.pconv_filter_similarity_order.restype = i
     lib.pconv_packed_mfma_blocks.argtypes = [vp, i, ctypes.POINTER(i), ctypes.POINTER(i)]
     lib.pconv_packed_mfma_blocks.restype = i
+    f, sz = ctypes.c_float, ctypes.POINTER(ctypes.c_size_t)
+    for name in ("pconv_linear_workspace", "pconv_linear_grad_input_workspace", "pconv_linear_grad_weight_workspace"):
+        getattr(lib, name).argtypes = [i, i, i, i, sz]
+    lib.pconv_linear.argtypes = [vp, ll, vp, ll, vp, vp, ll, vp, vp, ll, i, i, i, i, i, u, vp, ctypes.c_size_t, vp]
+    lib.pconv_linear_grad_input.argtypes = [vp, ll, vp, ll, vp, ll, i, vp, ll, vp, ll, i, i, i, i, vp, ctypes.c_size_t, vp]
+    lib.pconv_linear_grad_weight.argtypes = [vp, ll, vp, ll, vp, vp, i, i, i, i, vp, ctypes.c_size_t, vp]
+    lib.pconv_activation_grad.argtypes = [vp, ll, vp, ll, vp, ll, i, i, i, i, vp]
+    lib.pconv_layer_norm.argtypes = [vp, ll, vp, vp, f, vp, ll, vp, vp, i, i, i, vp]
+    lib.pconv_layer_norm_grad_workspace.argtypes = [i, i, i, sz]
+    lib.pconv_layer_norm_grad.argtypes = [vp, ll, vp, ll, vp, vp, vp, vp, ll, vp, vp, i, i, i, vp, ctypes.c_size_t, vp]
+    lib.pconv_distill.argtypes = [vp, ll, vp, vp, vp, vp, vp, ll, vp, i, i, i, i, f, vp]
+    lib.pconv_distill_grad.argtypes = [vp, ll, vp, vp, vp, vp, vp, ll, i, i, i, i, f, vp]
+    for name in ("pconv_linear_workspace", "pconv_linear_grad_input_workspace", "pconv_linear_grad_weight_workspace", "pconv_linear",
+                 "pconv_linear_grad_input", "pconv_linear_grad_weight", "pconv_activation_grad", "pconv_layer_norm",
+                 "pconv_layer_norm_grad_workspace", "pconv_layer_norm_grad", "pconv_distill", "pconv_distill_grad"):
+        getattr(lib, name).restype = i
     lib.pconv_strerror.argtypes = [i]
     lib.pconv_strerror.restype = ctypes.c_char_p
     lib.pconv_last_hip_error.argtypes = []
@@ -437,3 +456,81 @@ def packed_mfma_blocks(p: Packed, tile_filters: int):
     _check(_load().pconv_packed_mfma_blocks(p.handle, int(tile_filters), ctypes.byref(a), ctypes.byref(b)),
            "pconv_packed_mfma_blocks")
     return a.value, b.value
+
+
+# ---- pconv_dense.h: linear layers, layer norm, distillation; device tensors, row strides in elements (0: rows without gaps)
+
+def _bytes(name: str, *sizes: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(getattr(_load(), name)(*sizes, ctypes.byref(n)), name)
+    return n.value
+
+
+def linear_workspace(dtype: int, M: int, N: int, K: int) -> int:
+    return _bytes("pconv_linear_workspace", dtype, M, N, K)
+
+
+def linear(x, w, y, dtype: int, M: int, N: int, K: int, bias=None, residual=None, z=None, act: int = ACT_NONE, flags: int = 0,
+           ldx: int = 0, ldw: int = 0, ldr: int = 0, ldy: int = 0, workspace=None, workspace_bytes: int = 0, stream: int = 0):
+    """y = act(x w^T + bias) + residual, or act(x w^T + bias + residual) with FLAG_RESIDUAL_FIRST; z: the argument of act."""
+    _check(_load().pconv_linear(_dp(x), ldx, _dp(w), ldw, _dp(bias), _dp(residual), ldr, _dp(z), _dp(y), ldy, dtype, M, N, K, act,
+                                flags, _dp(workspace), workspace_bytes, stream or None), "pconv_linear")
+
+
+def linear_grad_input_workspace(dtype: int, M: int, N: int, K: int) -> int:
+    return _bytes("pconv_linear_grad_input_workspace", dtype, M, N, K)
+
+
+def linear_grad_input(dz, w, dx, dtype: int, M: int, N: int, K: int, z=None, act: int = ACT_NONE, add=None, lddz: int = 0, ldw: int = 0,
+                      ldz: int = 0, lda: int = 0, lddx: int = 0, workspace=None, workspace_bytes: int = 0, stream: int = 0):
+    """dx = (dz w) * act'(z) + add, z the argument of the activation that made x."""
+    _check(_load().pconv_linear_grad_input(_dp(dz), lddz, _dp(w), ldw, _dp(z), ldz, act, _dp(add), lda, _dp(dx), lddx, dtype, M, N, K,
+                                           _dp(workspace), workspace_bytes, stream or None), "pconv_linear_grad_input")
+
+
+def linear_grad_weight_workspace(dtype: int, M: int, N: int, K: int) -> int:
+    return _bytes("pconv_linear_grad_weight_workspace", dtype, M, N, K)
+
+
+def linear_grad_weight(dz, x, dw, dtype: int, M: int, N: int, K: int, db=None, lddz: int = 0, ldx: int = 0, workspace=None,
+                       workspace_bytes: int = 0, stream: int = 0):
+    """dw = dz^T x and db = column sums of dz, in fp32."""
+    _check(_load().pconv_linear_grad_weight(_dp(dz), lddz, _dp(x), ldx, _dp(dw), _dp(db), dtype, M, N, K, _dp(workspace),
+                                            workspace_bytes, stream or None), "pconv_linear_grad_weight")
+
+
+def activation_grad(dy, z, dz, dtype: int, M: int, N: int, act: int, lddy: int = 0, ldz: int = 0, lddz: int = 0, stream: int = 0):
+    """dz = dy * act'(z)."""
+    _check(_load().pconv_activation_grad(_dp(dy), lddy, _dp(z), ldz, _dp(dz), lddz, dtype, M, N, act, stream or None),
+           "pconv_activation_grad")
+
+
+def layer_norm(x, y, dtype: int, rows: int, D: int, gamma=None, beta=None, eps: float = 1e-5, mean=None, rstd=None, ldx: int = 0,
+               ldy: int = 0, stream: int = 0):
+    _check(_load().pconv_layer_norm(_dp(x), ldx, _dp(gamma), _dp(beta), eps, _dp(y), ldy, _dp(mean), _dp(rstd), dtype, rows, D,
+                                    stream or None), "pconv_layer_norm")
+
+
+def layer_norm_grad_workspace(dtype: int, rows: int, D: int) -> int:
+    return _bytes("pconv_layer_norm_grad_workspace", dtype, rows, D)
+
+
+def layer_norm_grad(dy, x, dx, mean, rstd, dtype: int, rows: int, D: int, gamma=None, dgamma=None, dbeta=None, lddy: int = 0,
+                    ldx: int = 0, lddx: int = 0, workspace=None, workspace_bytes: int = 0, stream: int = 0):
+    _check(_load().pconv_layer_norm_grad(_dp(dy), lddy, _dp(x), ldx, _dp(gamma), _dp(mean), _dp(rstd), _dp(dx), lddx, _dp(dgamma),
+                                         _dp(dbeta), dtype, rows, D, _dp(workspace), workspace_bytes, stream or None),
+           "pconv_layer_norm_grad")
+
+
+def distill(logits, indices, values, dtype: int, R: int, V: int, k: int, temperature: float, weight=None, loss=None, grad=None,
+            stats=None, ldl: int = 0, ldg: int = 0, stream: int = 0):
+    """Loss of every row against the teacher's k top logits, and the gradient of the logits."""
+    _check(_load().pconv_distill(_dp(logits), ldl, _dp(indices), _dp(values), _dp(weight), _dp(loss), _dp(grad), ldg, _dp(stats), dtype,
+                                 R, V, k, temperature, stream or None), "pconv_distill")
+
+
+def distill_grad(logits, indices, values, stats, grad, dtype: int, R: int, V: int, k: int, temperature: float, weight=None,
+                 ldl: int = 0, ldg: int = 0, stream: int = 0):
+    """The gradient alone, from the stats that distill left; weight: the gradient of every row's loss."""
+    _check(_load().pconv_distill_grad(_dp(logits), ldl, _dp(indices), _dp(values), _dp(weight), _dp(stats), _dp(grad), ldg, dtype, R, V,
+                                      k, temperature, stream or None), "pconv_distill_grad")

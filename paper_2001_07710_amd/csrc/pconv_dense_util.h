@@ -1,0 +1,186 @@
+// Shared by the operators of pconv_dense.h (pconv_linear*.hip, pconv_norm.hip, pconv_distill.hip): storage types, 16-byte
+// pieces of rows at any alignment, activations, checks of arguments.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <cstring>
+
+#include "pconv_dense.h"
+#include "pconv_internal.h"
+#include "pconv_mfma_util.h"
+
+#define PCONV_HIP(call)                                  \
+    do {                                                 \
+        hipError_t e_ = (call);                          \
+        if (e_ != hipSuccess) {                          \
+            ::pconv::set_hip_error(#call, (int)e_);      \
+            return PCONV_EHIP;                           \
+        }                                                \
+    } while (0)
+
+namespace pconv {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short short4v __attribute__((ext_vector_type(4)));
+
+// A storage type: its element, and how many of them a 16-byte piece holds.
+template <int DT>
+struct Store;
+template <>
+struct Store<PCONV_F32> {
+    typedef float T;
+    typedef float4v V;
+    static constexpr int kPer = 4;
+};
+template <>
+struct Store<PCONV_F16> {
+    typedef _Float16 T;
+    typedef half8 V;
+    static constexpr int kPer = 8;
+};
+template <>
+struct Store<PCONV_BF16> {
+    typedef __bf16 T;
+    typedef bf16x8 V;
+    static constexpr int kPer = 8;
+};
+
+inline int elem_bytes(int dtype) { return dtype == PCONV_F32 ? 4 : 2; }
+
+// 16 bytes from / to an address that is aligned to one element only: one wide access (the hardware takes any alignment).
+__device__ __forceinline__ uint4v load16(const void* p) {
+    uint4v v;
+    __builtin_memcpy(&v, p, 16);
+    return v;
+}
+__device__ __forceinline__ void store16(void* p, uint4v v) { __builtin_memcpy(p, &v, 16); }
+
+// The first n elements of a piece, zeros behind them; nothing behind them is read.
+template <int DT>
+__device__ __forceinline__ uint4v load_part(const typename Store<DT>::T* p, int n) {
+    constexpr int P = Store<DT>::kPer;
+    if (n >= P) return load16(p);
+    typename Store<DT>::V v = {};
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+        if (i < n) v[i] = p[i];
+    return __builtin_bit_cast(uint4v, v);
+}
+
+// Eight consecutive values, as stored, and as floats; `n` of them are there.
+template <int DT>
+struct Eight {
+    static constexpr int P = Store<DT>::kPer;
+    uint4v raw[8 / P];
+    __device__ __forceinline__ void load(const typename Store<DT>::T* p, int n) {
+#pragma unroll
+        for (int h = 0; h < 8 / P; ++h) raw[h] = load_part<DT>(p + h * P, n - h * P);
+    }
+    __device__ __forceinline__ void get(float out[8]) const {
+#pragma unroll
+        for (int h = 0; h < 8 / P; ++h) {
+            const auto v = __builtin_bit_cast(typename Store<DT>::V, raw[h]);
+#pragma unroll
+            for (int i = 0; i < P; ++i) out[h * P + i] = (float)v[i];
+        }
+    }
+};
+template <int DT>
+__device__ __forceinline__ void load8(const typename Store<DT>::T* p, int n, float out[8]) {
+    Eight<DT> e;
+    e.load(p, n);
+    e.get(out);
+}
+// Eight consecutive values from floats, rounded once; the first n of them are stored.
+template <int DT>
+__device__ __forceinline__ void store8(typename Store<DT>::T* p, int n, const float in[8]) {
+    typedef typename Store<DT>::T T;
+    constexpr int P = Store<DT>::kPer;
+#pragma unroll
+    for (int h = 0; h < 8 / P; ++h) {
+        typename Store<DT>::V v;
+#pragma unroll
+        for (int i = 0; i < P; ++i) v[i] = (T)in[h * P + i];
+        if (n >= (h + 1) * P) {
+            store16(p + h * P, __builtin_bit_cast(uint4v, v));
+        } else {
+#pragma unroll
+            for (int i = 0; i < P; ++i)
+                if (h * P + i < n) p[h * P + i] = v[i];
+        }
+    }
+}
+
+constexpr float kSqrtHalf = 0.70710678118654752f, kSqrt2OverPi = 0.79788456080286536f, kInvSqrt2Pi = 0.39894228040143268f;
+
+// z moved into +-100, NaN left as it is: behind that an activation's curve is 0 or 1 (times z) in 32 bits, and no inf * 0 arises
+__device__ __forceinline__ float tamed(float z) { return z > 100.f ? 100.f : z < -100.f ? -100.f : z; }
+
+__device__ __forceinline__ float relu(float z) { return z < 0.f ? 0.f : z; }                    // (NaN stays)
+__device__ __forceinline__ float relu_slope(float z) { return z > 0.f ? 1.f : z == z ? 0.f : z; }
+__device__ __forceinline__ float gelu(float z) { return z * (0.5f + 0.5f * erff(tamed(z) * kSqrtHalf)); }
+__device__ __forceinline__ float gelu_slope(float z) {
+    const float t = tamed(z);
+    return 0.5f + 0.5f * erff(t * kSqrtHalf) + t * kInvSqrt2Pi * __expf(-0.5f * t * t);
+}
+// (1 + tanh(u)) / 2 = 1 / (1 + exp(-2u)): no cancellation where the curve nears 0
+__device__ __forceinline__ float gelu_tanh_share(float t) {
+    return 1.f / (1.f + __expf(-2.f * kSqrt2OverPi * (t + 0.044715f * t * t * t)));
+}
+__device__ __forceinline__ float gelu_tanh(float z) { return z * gelu_tanh_share(tamed(z)); }
+__device__ __forceinline__ float gelu_tanh_slope(float z) {
+    const float t = tamed(z), s = gelu_tanh_share(t);
+    return s + t * s * (1.f - s) * (2.f * kSqrt2OverPi) * (1.f + 3.f * 0.044715f * t * t);
+}
+__device__ __forceinline__ float silu(float z) { return z * (1.f / (1.f + __expf(-tamed(z)))); }
+__device__ __forceinline__ float silu_slope(float z) {
+    const float t = tamed(z), s = 1.f / (1.f + __expf(-t));
+    return s * (1.f + t * (1.f - s));
+}
+
+// v[q] = curve(v[q]), or v[q] *= slope(z[q])
+__device__ __forceinline__ void activate8(float v[8], int act) {
+#define PCONV_EACH(F)                                   \
+    _Pragma("unroll") for (int q = 0; q < 8; ++q) v[q] = F(v[q]); \
+    break
+    switch (act) {
+        case PCONV_ACT_RELU: PCONV_EACH(relu);
+        case PCONV_ACT_GELU: PCONV_EACH(gelu);
+        case PCONV_ACT_GELU_TANH: PCONV_EACH(gelu_tanh);
+        case PCONV_ACT_SILU: PCONV_EACH(silu);
+        default: break;
+    }
+#undef PCONV_EACH
+}
+__device__ __forceinline__ void times_slope8(float v[8], const float z[8], int act) {
+#define PCONV_EACH(F)                                   \
+    _Pragma("unroll") for (int q = 0; q < 8; ++q) v[q] *= F(z[q]); \
+    break
+    switch (act) {
+        case PCONV_ACT_RELU: PCONV_EACH(relu_slope);
+        case PCONV_ACT_GELU: PCONV_EACH(gelu_slope);
+        case PCONV_ACT_GELU_TANH: PCONV_EACH(gelu_tanh_slope);
+        case PCONV_ACT_SILU: PCONV_EACH(silu_slope);
+        default: break;
+    }
+#undef PCONV_EACH
+}
+
+constexpr long long kMostStride = 1 << 20;
+
+inline bool is_dtype(int dtype) { return dtype == PCONV_F32 || dtype == PCONV_F16 || dtype == PCONV_BF16; }
+inline bool aligned_to(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+// A matrix's row stride: 0 becomes `cols`
+inline int check_stride(long long* ld, int cols) {
+    if (*ld == 0) *ld = cols;
+    if (*ld < cols) return PCONV_ESHAPE;
+    if (*ld > kMostStride) return PCONV_EUNSUPPORTED;
+    return PCONV_OK;
+}
+
+}  // namespace
+}  // namespace pconv

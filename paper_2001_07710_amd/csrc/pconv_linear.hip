@@ -1,0 +1,292 @@
+// Entry points of the matrix products of pconv_dense.h: checks, the choice of tile and of how many workgroups share a tile, the
+// column sums of the bias gradient, the gradient in front of an activation.  The products themselves: pconv_linear_kernels.h.
+#include "pconv_dense_util.h"
+#include "pconv_linear.h"
+
+namespace pconv {
+namespace {
+
+constexpr int kMostRows = 1 << 30;          // (the kernels count rows, and stages of a product over rows, in 32 bits)
+constexpr int kComputeUnits = 256;          // of an MI355X: plans and workspaces are the same whatever device is current
+
+struct Plan {
+    int tile = 0;                           // kTiles: the kernel for few rows
+    int splits = 1, c_per = 0;
+    size_t part_bytes = 0;
+};
+
+// Tile and split of a product of I x J results over C.
+Plan plan_product(int dtype, int I, int J, int C, bool forward) {
+    Plan p;
+    const int stage = kStageBytes / elem_bytes(dtype);
+    const int stages = (C + stage - 1) / stage;
+    long long tiles = 0, wanted = 0;
+    if (forward && I <= kFewRows) {
+        p.tile = kTiles;
+        tiles = (J + 15ll) / 16;
+        wanted = 64;
+    } else {
+        for (p.tile = 0; p.tile < kTiles; ++p.tile) {
+            const TileShape& s = kTileShapes[p.tile];
+            tiles = ((I + (long long)s.i - 1) / s.i) * ((J + (long long)s.j - 1) / s.j);
+            if (tiles >= (p.tile == 0 ? 192 : 256) || p.tile == kTiles - 1) break;
+        }
+        wanted = kComputeUnits;
+    }
+    long long splits = tiles >= wanted ? 1 : wanted / tiles;
+    splits = std::max(1ll, std::min({splits, (long long)stages / 4, 32ll}));
+    const int per = (int)((stages + splits - 1) / splits);
+    p.splits = (stages + per - 1) / per;
+    p.c_per = per * stage;
+    if (p.splits > 1) p.part_bytes = (size_t)p.splits * (size_t)I * (size_t)J * sizeof(float);
+    return p;
+}
+
+int launch(int dtype, const Product& p, bool few, void* stream) {
+    switch (dtype) {
+        case PCONV_F32: return few ? launch_few_rows_f32(p, stream) : launch_product_f32(p, stream);
+        case PCONV_F16: return few ? launch_few_rows_f16(p, stream) : launch_product_f16(p, stream);
+        default: return few ? launch_few_rows_bf16(p, stream) : launch_product_bf16(p, stream);
+    }
+}
+
+int run(int dtype, Product& p, const Plan& plan, void* workspace, void* stream) {
+    p.tile = plan.tile;
+    p.splits = plan.splits;
+    p.c_per = plan.c_per;
+    p.parts = static_cast<float*>(workspace);
+    return launch(dtype, p, plan.tile == kTiles, stream);
+}
+
+int check_sizes(int dtype, int M, int N, int K) {
+    if (!is_dtype(dtype)) return PCONV_EINVAL;
+    if (M < 0 || N < 1 || K < 1) return PCONV_ESHAPE;
+    if (M > kMostRows || N > kMostStride || K > kMostStride) return PCONV_EUNSUPPORTED;
+    return PCONV_OK;
+}
+bool bad_element_alignment(int dtype, const void* p) { return !aligned_to(p, elem_bytes(dtype)); }
+bool bad_act(int act) { return act < PCONV_ACT_NONE || act > PCONV_ACT_SILU; }
+bool bad_workspace(const void* ws, size_t have, size_t need) { return need && (!ws || have < need || !aligned_to(ws, 16)); }
+
+// ---- column sums of dz (the bias gradient): a workgroup sums a strip of rows for 512 columns, in the order of the rows
+constexpr int kSumCols = 512, kMostStrips = 64;
+int sum_strips(int M, int N) {
+    const int wide = (N + kSumCols - 1) / kSumCols;
+    return std::max(1, std::min({kMostStrips, (int)((M + 63ll) / 64), (2 * kComputeUnits + wide - 1) / wide}));
+}
+
+template <int DT>
+__global__ __launch_bounds__(256) void column_sums_kernel(const typename Store<DT>::T* m, long long ld, int M, int N, int per, float* out) {
+    __shared__ __align__(16) float part[3][kSumCols];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int j = blockIdx.x * kSumCols + lane * 8, n = N - j;
+    const long long r0 = (long long)blockIdx.y * per, r1 = min((long long)M, r0 + per);
+    float sum[8] = {}, v[8];
+    if (n > 0)
+#pragma unroll 4
+        for (long long r = r0 + wave; r < r1; r += 4) {
+            load8<DT>(m + r * ld + j, n, v);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) sum[q] += v[q];
+        }
+    if (wave) store8<PCONV_F32>(&part[wave - 1][lane * 8], 8, sum);
+    __syncthreads();
+    if (wave == 0 && n > 0) {
+        for (int s = 0; s < 3; ++s)
+#pragma unroll
+            for (int q = 0; q < 8; ++q) sum[q] += part[s][lane * 8 + q];
+        store8<PCONV_F32>(out + (size_t)blockIdx.y * N + j, n, sum);
+    }
+}
+__global__ __launch_bounds__(256) void add_strips_kernel(const float* parts, int strips, int N, float* out) {
+    const int j = blockIdx.x * 256 + threadIdx.x;
+    if (j >= N) return;
+    float sum = 0.f;
+    for (int s = 0; s < strips; ++s) sum += parts[(size_t)s * N + j];
+    out[j] = sum;
+}
+__global__ __launch_bounds__(256) void fill_zero_kernel(float* out, unsigned long long n) {
+    const unsigned long long i = (unsigned long long)blockIdx.x * 256 + threadIdx.x;
+    if (i < n) out[i] = 0.f;
+}
+
+template <int DT>
+int column_sums(const void* m, long long ld, int M, int N, float* parts, float* out, hipStream_t st) {
+    const int strips = sum_strips(M, N), per = (M + strips - 1) / strips;
+    hipLaunchKernelGGL(column_sums_kernel<DT>, dim3((N + kSumCols - 1) / kSumCols, strips), dim3(256), 0, st,
+                       static_cast<const typename Store<DT>::T*>(m), ld, M, N, per, strips > 1 ? parts : out);
+    PCONV_HIP(hipGetLastError());
+    if (strips > 1) {
+        hipLaunchKernelGGL(add_strips_kernel, dim3((N + 255) / 256), dim3(256), 0, st, parts, strips, N, out);
+        PCONV_HIP(hipGetLastError());
+    }
+    return PCONV_OK;
+}
+size_t strip_bytes(int M, int N) {
+    const int strips = sum_strips(M, N);
+    return strips > 1 ? ((size_t)strips * N * sizeof(float) + 15) / 16 * 16 : 0;
+}
+
+template <int DT>
+__global__ __launch_bounds__(256) void activation_grad_kernel(const typename Store<DT>::T* dy, long long lddy, const typename Store<DT>::T* z,
+                                                              long long ldz, typename Store<DT>::T* dz, long long lddz, int M, int N, int act) {
+    const unsigned per_row = (unsigned)(N + 7) / 8;
+    const unsigned long long at = (unsigned long long)blockIdx.x * 256 + threadIdx.x, i = at / per_row;
+    if (i >= (unsigned long long)M) return;
+    const int j = (int)(at % per_row) * 8, n = N - j;
+    float v[8], a[8];
+    load8<DT>(dy + i * lddy + j, n, v);
+    load8<DT>(z + i * ldz + j, n, a);
+    times_slope8(v, a, act);
+    store8<DT>(dz + i * lddz + j, n, v);
+}
+
+template <int DT>
+int activation_grad(const void* dy, long long lddy, const void* z, long long ldz, void* dz, long long lddz, int M, int N, int act, hipStream_t st) {
+    typedef typename Store<DT>::T T;
+    const unsigned long long blocks = ((unsigned long long)M * ((N + 7ll) / 8) + 255) / 256;
+    if (blocks > 0x7FFFFFFFull) return PCONV_EUNSUPPORTED;
+    hipLaunchKernelGGL(activation_grad_kernel<DT>, dim3((unsigned)blocks), dim3(256), 0, st, static_cast<const T*>(dy), lddy,
+                       static_cast<const T*>(z), ldz, static_cast<T*>(dz), lddz, M, N, act);
+    PCONV_HIP(hipGetLastError());
+    return PCONV_OK;
+}
+
+}  // namespace
+}  // namespace pconv
+
+using namespace pconv;
+
+extern "C" int pconv_linear_workspace(int dtype, int M, int N, int K, size_t* bytes) {
+    if (!bytes) return PCONV_EINVAL;
+    *bytes = 0;
+    if (int rc = check_sizes(dtype, M, N, K)) return rc;
+    if (M > 0) *bytes = plan_product(dtype, M, N, K, true).part_bytes;
+    return PCONV_OK;
+}
+
+extern "C" int pconv_linear(const void* x, long long ldx, const void* w, long long ldw, const float* bias, const void* residual,
+                            long long ldr, void* z, void* y, long long ldy, int dtype, int M, int N, int K, int act, unsigned flags,
+                            void* workspace, size_t workspace_bytes, void* stream) {
+    if (int rc = check_sizes(dtype, M, N, K)) return rc;
+    if (bad_act(act) || (flags & ~(unsigned)PCONV_FLAG_RESIDUAL_FIRST)) return PCONV_EINVAL;
+    for (int rc : {check_stride(&ldx, K), check_stride(&ldw, K), residual ? check_stride(&ldr, N) : PCONV_OK, check_stride(&ldy, N)})
+        if (rc) return rc;
+    if (M == 0) return PCONV_OK;
+    if (!x || !w || !y) return PCONV_EINVAL;
+    for (const void* p : {x, w, residual, (const void*)z, (const void*)y})
+        if (bad_element_alignment(dtype, p)) return PCONV_EINVAL;
+    if (!aligned_to(bias, 4)) return PCONV_EINVAL;
+    const Plan plan = plan_product(dtype, M, N, K, true);
+    if (bad_workspace(workspace, workspace_bytes, plan.part_bytes)) return PCONV_EINVAL;
+    Product p{};
+    p.a = x; p.lda = ldx; p.b = w; p.ldb = ldw;
+    p.I = M; p.J = N; p.C = K;
+    p.f.kind = kForward;
+    p.f.act = act;
+    p.f.first = (flags & PCONV_FLAG_RESIDUAL_FIRST) != 0;
+    p.f.bias = bias;
+    p.f.add = residual; p.f.ld_add = ldr;
+    p.f.z = z;
+    p.f.out = y; p.f.ld_out = ldy;
+    return run(dtype, p, plan, workspace, stream);
+}
+
+extern "C" int pconv_linear_grad_input_workspace(int dtype, int M, int N, int K, size_t* bytes) {
+    if (!bytes) return PCONV_EINVAL;
+    *bytes = 0;
+    if (int rc = check_sizes(dtype, M, N, K)) return rc;
+    if (M > 0) *bytes = plan_product(dtype, M, K, N, false).part_bytes;
+    return PCONV_OK;
+}
+
+extern "C" int pconv_linear_grad_input(const void* dz, long long lddz, const void* w, long long ldw, const void* z, long long ldz,
+                                       int act, const void* add, long long lda, void* dx, long long lddx, int dtype, int M, int N,
+                                       int K, void* workspace, size_t workspace_bytes, void* stream) {
+    if (int rc = check_sizes(dtype, M, N, K)) return rc;
+    if (bad_act(act) || (act != PCONV_ACT_NONE && !z && M > 0)) return PCONV_EINVAL;
+    for (int rc : {check_stride(&lddz, N), check_stride(&ldw, K), z ? check_stride(&ldz, K) : PCONV_OK,
+                   add ? check_stride(&lda, K) : PCONV_OK, check_stride(&lddx, K)})
+        if (rc) return rc;
+    if (M == 0) return PCONV_OK;
+    if (!dz || !w || !dx) return PCONV_EINVAL;
+    for (const void* p : {dz, w, z, add, (const void*)dx})
+        if (bad_element_alignment(dtype, p)) return PCONV_EINVAL;
+    const Plan plan = plan_product(dtype, M, K, N, false);
+    if (bad_workspace(workspace, workspace_bytes, plan.part_bytes)) return PCONV_EINVAL;
+    Product p{};
+    p.a = dz; p.lda = lddz; p.b = w; p.ldb = ldw;
+    p.I = M; p.J = K; p.C = N;
+    p.b_rows = true;
+    p.f.kind = kGradInput;
+    p.f.act = act;
+    p.f.zin = act == PCONV_ACT_NONE ? nullptr : z; p.f.ld_zin = ldz;
+    p.f.add = add; p.f.ld_add = lda;
+    p.f.out = dx; p.f.ld_out = lddx;
+    return run(dtype, p, plan, workspace, stream);
+}
+
+extern "C" int pconv_linear_grad_weight_workspace(int dtype, int M, int N, int K, size_t* bytes) {
+    if (!bytes) return PCONV_EINVAL;
+    *bytes = 0;
+    if (int rc = check_sizes(dtype, M, N, K)) return rc;
+    // (the strips of the bias gradient's sums first, the product's parts behind them)
+    if (M > 0) *bytes = strip_bytes(M, N) + plan_product(dtype, N, K, M, false).part_bytes;
+    return PCONV_OK;
+}
+
+extern "C" int pconv_linear_grad_weight(const void* dz, long long lddz, const void* x, long long ldx, float* dw, float* db, int dtype,
+                                        int M, int N, int K, void* workspace, size_t workspace_bytes, void* stream) {
+    if (int rc = check_sizes(dtype, M, N, K)) return rc;
+    for (int rc : {check_stride(&lddz, N), check_stride(&ldx, K)})
+        if (rc) return rc;
+    if (!dw || !aligned_to(dw, 4) || !aligned_to(db, 4)) return PCONV_EINVAL;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (M == 0) {
+        const unsigned long long n = (unsigned long long)N * K;
+        if ((n + 255) / 256 > 0x7FFFFFFFull) return PCONV_EUNSUPPORTED;
+        hipLaunchKernelGGL(fill_zero_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, dw, n);
+        PCONV_HIP(hipGetLastError());
+        if (db) {
+            hipLaunchKernelGGL(fill_zero_kernel, dim3((N + 255) / 256), dim3(256), 0, st, db, (unsigned long long)N);
+            PCONV_HIP(hipGetLastError());
+        }
+        return PCONV_OK;
+    }
+    if (!dz || !x) return PCONV_EINVAL;
+    for (const void* p : {dz, x})
+        if (bad_element_alignment(dtype, p)) return PCONV_EINVAL;
+    const Plan plan = plan_product(dtype, N, K, M, false);
+    const size_t strips = strip_bytes(M, N);
+    if (bad_workspace(workspace, workspace_bytes, strips + plan.part_bytes)) return PCONV_EINVAL;
+    if (db) {
+        float* const parts = static_cast<float*>(workspace);
+        int rc = dtype == PCONV_F32   ? column_sums<PCONV_F32>(dz, lddz, M, N, parts, db, st)
+                 : dtype == PCONV_F16 ? column_sums<PCONV_F16>(dz, lddz, M, N, parts, db, st)
+                                      : column_sums<PCONV_BF16>(dz, lddz, M, N, parts, db, st);
+        if (rc) return rc;
+    }
+    Product p{};
+    p.a = dz; p.lda = lddz; p.b = x; p.ldb = ldx;
+    p.I = N; p.J = K; p.C = M;
+    p.a_rows = p.b_rows = true;
+    p.f.kind = kFloat;
+    p.f.out = dw; p.f.ld_out = K;
+    return run(dtype, p, plan, workspace ? static_cast<char*>(workspace) + strips : nullptr, stream);
+}
+
+extern "C" int pconv_activation_grad(const void* dy, long long lddy, const void* z, long long ldz, void* dz, long long lddz, int dtype,
+                                     int M, int N, int act, void* stream) {
+    if (int rc = check_sizes(dtype, M, N, 1)) return rc;
+    if (bad_act(act)) return PCONV_EINVAL;
+    for (int rc : {check_stride(&lddy, N), check_stride(&ldz, N), check_stride(&lddz, N)})
+        if (rc) return rc;
+    if (M == 0) return PCONV_OK;
+    if (!dy || !z || !dz) return PCONV_EINVAL;
+    for (const void* p : {dy, z, (const void*)dz})
+        if (bad_element_alignment(dtype, p)) return PCONV_EINVAL;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return dtype == PCONV_F32   ? activation_grad<PCONV_F32>(dy, lddy, z, ldz, dz, lddz, M, N, act, st)
+           : dtype == PCONV_F16 ? activation_grad<PCONV_F16>(dy, lddy, z, ldz, dz, lddz, M, N, act, st)
+                                : activation_grad<PCONV_BF16>(dy, lddy, z, ldz, dz, lddz, M, N, act, st);
+}
