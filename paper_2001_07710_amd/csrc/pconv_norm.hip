@@ -19,28 +19,27 @@ __device__ __forceinline__ float lanes_sum(float v) {
     return v;
 }
 
-// Sums of two values over the TPR threads that hold a row.  `room`: 2 * waves floats of LDS for each of two turns, used in turn,
-// so that one barrier a sum is enough.
-template <int TPR>
+// Sums of N values over the TPR threads that hold a row (of THREADS that meet at the barrier).  The waves' sums lie in one half of
+// `room` or the other by turns, so that one barrier is enough.
+template <int TPR, int N>
 struct RowSum {
-    float (*room)[2][16];
+    float (*room)[N][16];
     int turn = 0;
-    __device__ __forceinline__ void operator()(float& a, float& b) {
-        a = lanes_sum<(TPR < 64 ? TPR : 64)>(a);
-        b = lanes_sum<(TPR < 64 ? TPR : 64)>(b);
+    __device__ __forceinline__ void operator()(float (&v)[N]) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) v[n] = lanes_sum<(TPR < 64 ? TPR : 64)>(v[n]);
         if constexpr (TPR > 64) {
             constexpr int W = TPR / 64;
             const int wave = threadIdx.x >> 6, first = wave / W * W;
-            if ((threadIdx.x & 63) == 0) {
-                room[turn][0][wave] = a;
-                room[turn][1][wave] = b;
-            }
-            __syncthreads();
-            a = b = 0.f;
+            if ((threadIdx.x & 63) == 0)
 #pragma unroll
-            for (int w = 0; w < W; ++w) {
-                a += room[turn][0][first + w];
-                b += room[turn][1][first + w];
+                for (int n = 0; n < N; ++n) room[turn][n][wave] = v[n];
+            __syncthreads();
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                v[n] = 0.f;
+#pragma unroll
+                for (int w = 0; w < W; ++w) v[n] += room[turn][n][first + w];
             }
             turn ^= 1;
         }
@@ -62,14 +61,34 @@ struct NormArgs {
     float eps;
 };
 
-template <int DT, int TPR, int Q, int THREADS>
+// One reading of a thread's pieces of U rows, asked for one turn ahead of their use.
+template <int DT, int TPR, int Q, int U>
+struct Rows {
+    uint4v raw[U][Q];
+    __device__ __forceinline__ void load(const void* m, long long ld, long long r, long long between, int rows, int D, int t) {
+        constexpr int P = Store<DT>::kPer;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const bool there = r + u * between < rows;
+            const auto* const at = static_cast<const typename Store<DT>::T*>(m) + (there ? r + u * between : 0) * ld;
+#pragma unroll
+            for (int q = 0; q < Q; ++q) raw[u][q] = load_part<DT>(at + (t + q * TPR) * P, there ? D - (t + q * TPR) * P : 0);
+        }
+    }
+};
+
+template <int DT, int TPR, int Q, int U, int THREADS>
 __global__ __launch_bounds__(THREADS) void norm_kernel(const NormArgs p) {
     typedef typename Store<DT>::T T;
     typedef typename Store<DT>::V V;
     constexpr int P = Store<DT>::kPer, GROUPS = THREADS / TPR;
-    __shared__ float room[2][2][16];
-    RowSum<TPR> row_sum{room};
+    __shared__ float room[2][U][16];
+    RowSum<TPR, U> row_sum{room};
     const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
+    const long long step = (long long)gridDim.x * GROUPS, first = (long long)blockIdx.x * GROUPS + group;
+    const long long turns = (p.rows + step * U - 1) / (step * U);    // (the same for every thread: row_sum has barriers)
+    Rows<DT, TPR, Q, U> rows;
+    rows.load(p.x, p.ldx, first, step, p.rows, p.D, t);
     float gamma[Q][P], beta[Q][P];
 #pragma unroll
     for (int q = 0; q < Q; ++q)
@@ -80,68 +99,91 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const NormArgs p) {
             beta[q][e] = d < p.D && p.beta ? p.beta[d] : 0.f;
         }
     const float inv = 1.f / (float)p.D;
-    const long long step = (long long)gridDim.x * GROUPS;
-    const long long turns = (p.rows + step - 1) / step;         // (the same for every thread: row_sum has barriers)
     for (long long k = 0; k < turns; ++k) {
-        const long long r = k * step + (long long)blockIdx.x * GROUPS + group;
-        const bool there = r < p.rows;
-        const T* const x = static_cast<const T*>(p.x) + (there ? r : 0) * p.ldx;
-        uint4v raw[Q];
+        const long long r0 = k * step * U + first;
+        // (the next rows are under way while these are worked on, where registers are left for them)
+        constexpr bool AHEAD = Q < 4;
+        if (!AHEAD && k) rows.load(p.x, p.ldx, r0, step, p.rows, p.D, t);
+        const Rows<DT, TPR, Q, U> now = rows;
+        if (AHEAD && k + 1 < turns) rows.load(p.x, p.ldx, r0 + step * U, step, p.rows, p.D, t);
+        float mean[U], rstd[U];
 #pragma unroll
-        for (int q = 0; q < Q; ++q) raw[q] = load_part<DT>(x + (t + q * TPR) * P, there ? p.D - (t + q * TPR) * P : 0);
-        float sum = 0.f, none = 0.f;
+        for (int u = 0; u < U; ++u) {
+            mean[u] = 0.f;
 #pragma unroll
-        for (int q = 0; q < Q; ++q) {
-            const V v = __builtin_bit_cast(V, raw[q]);
+            for (int q = 0; q < Q; ++q) {
+                const V v = __builtin_bit_cast(V, now.raw[u][q]);
 #pragma unroll
-            for (int e = 0; e < P; ++e) sum += (float)v[e];
-        }
-        row_sum(sum, none);
-        const float mean = sum * inv;
-        float squares = 0.f;
-        none = 0.f;
-#pragma unroll
-        for (int q = 0; q < Q; ++q) {
-            const V v = __builtin_bit_cast(V, raw[q]);
-#pragma unroll
-            for (int e = 0; e < P; ++e) {
-                const float d = (float)v[e] - mean;
-                squares += (t + q * TPR) * P + e < p.D ? d * d : 0.f;
+                for (int e = 0; e < P; ++e) mean[u] += (float)v[e];
             }
         }
-        row_sum(squares, none);
-        const float rstd = 1.f / sqrtf(squares * inv + p.eps);
-        if (!there) continue;
-        if (t == 0) {
-            if (p.mean) p.mean[r] = mean;
-            if (p.rstd) p.rstd[r] = rstd;
+        row_sum(mean);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            mean[u] *= inv;
+            rstd[u] = 0.f;
+#pragma unroll
+            for (int q = 0; q < Q; ++q) {
+                const V v = __builtin_bit_cast(V, now.raw[u][q]);
+#pragma unroll
+                for (int e = 0; e < P; ++e) {
+                    const float d = (float)v[e] - mean[u];
+                    rstd[u] += (t + q * TPR) * P + e < p.D ? d * d : 0.f;
+                }
+            }
         }
-        T* const y = static_cast<T*>(p.out) + r * p.ldo;
+        row_sum(rstd);
 #pragma unroll
-        for (int q = 0; q < Q; ++q) {
-            const V v = __builtin_bit_cast(V, raw[q]);
-            const int d = (t + q * TPR) * P, n = p.D - d;
-            V o;
+        for (int u = 0; u < U; ++u) {
+            const long long r = r0 + u * step;
+            if (r >= p.rows) break;
+            rstd[u] = 1.f / sqrtf(rstd[u] * inv + p.eps);
+            if (t == 0) {
+                if (p.mean) p.mean[r] = mean[u];
+                if (p.rstd) p.rstd[r] = rstd[u];
+            }
+            T* const y = static_cast<T*>(p.out) + r * p.ldo;
 #pragma unroll
-            for (int e = 0; e < P; ++e) o[e] = (T)(((float)v[e] - mean) * rstd * gamma[q][e] + beta[q][e]);
-            if (n >= P) store16(y + d, __builtin_bit_cast(uint4v, o));
-            else
+            for (int q = 0; q < Q; ++q) {
+                const V v = __builtin_bit_cast(V, now.raw[u][q]);
+                const int d = (t + q * TPR) * P, n = p.D - d;
+                V o;
 #pragma unroll
-                for (int e = 0; e < P; ++e)
-                    if (e < n) y[d + e] = o[e];
+                for (int e = 0; e < P; ++e) o[e] = (T)(((float)v[e] - mean[u]) * rstd[u] * gamma[q][e] + beta[q][e]);
+                if (n >= P) store16(y + d, __builtin_bit_cast(uint4v, o));
+                else
+#pragma unroll
+                    for (int e = 0; e < P; ++e)
+                        if (e < n) y[d + e] = o[e];
+            }
         }
     }
 }
 
-template <int DT, int TPR, int Q, int THREADS>
+template <int DT, int TPR, int Q, int U, int THREADS>
 __global__ __launch_bounds__(THREADS) void norm_grad_kernel(const NormArgs p) {
     typedef typename Store<DT>::T T;
     typedef typename Store<DT>::V V;
     constexpr int P = Store<DT>::kPer, GROUPS = THREADS / TPR;
-    __shared__ float room[2][2][16];
+    __shared__ float room[2][2 * U][16];
     __shared__ __align__(16) float columns[GROUPS > 1 ? THREADS * P : 1];
-    RowSum<TPR> row_sum{room};
+    RowSum<TPR, 2 * U> row_sum{room};
     const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
+    const long long step = (long long)gridDim.x * GROUPS, first = (long long)blockIdx.x * GROUPS + group;
+    const long long turns = (p.rows + step * U - 1) / (step * U);
+    Rows<DT, TPR, Q, U> xs, dys;
+    float mean_next[U], rstd_next[U];
+    auto load = [&](long long r) {
+        xs.load(p.x, p.ldx, r, step, p.rows, p.D, t);
+        dys.load(p.dy, p.lddy, r, step, p.rows, p.D, t);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const bool there = r + u * step < p.rows;
+            mean_next[u] = there ? p.mean[r + u * step] : 0.f;
+            rstd_next[u] = there ? p.rstd[r + u * step] : 0.f;
+        }
+    };
+    load(first);
     float gamma[Q][P], dg[Q][P], db[Q][P];
 #pragma unroll
     for (int q = 0; q < Q; ++q)
@@ -152,55 +194,61 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(const NormArgs p) {
             dg[q][e] = db[q][e] = 0.f;
         }
     const float inv = 1.f / (float)p.D;
-    const long long step = (long long)gridDim.x * GROUPS;
-    const long long turns = (p.rows + step - 1) / step;
     for (long long k = 0; k < turns; ++k) {
-        const long long r = k * step + (long long)blockIdx.x * GROUPS + group;
-        const bool there = r < p.rows;
-        const T* const x = static_cast<const T*>(p.x) + (there ? r : 0) * p.ldx;
-        const T* const dy = static_cast<const T*>(p.dy) + (there ? r : 0) * p.lddy;
-        uint4v rx[Q], rd[Q];
+        const long long r0 = k * step * U + first;
+        constexpr bool AHEAD = THREADS < 1024;
+        if (!AHEAD && k) load(r0);
+        const Rows<DT, TPR, Q, U> x = xs, dy = dys;
+        float mean[U], rstd[U], s[2 * U];
 #pragma unroll
-        for (int q = 0; q < Q; ++q) {
-            const int d = (t + q * TPR) * P, n = there ? p.D - d : 0;
-            rx[q] = load_part<DT>(x + d, n);
-            rd[q] = load_part<DT>(dy + d, n);
+        for (int u = 0; u < U; ++u) {
+            mean[u] = mean_next[u];
+            rstd[u] = rstd_next[u];
         }
-        const float mean = there ? p.mean[r] : 0.f, rstd = there ? p.rstd[r] : 0.f;
-        float s1 = 0.f, s2 = 0.f;
+        if (AHEAD && k + 1 < turns) load(r0 + step * U);
 #pragma unroll
-        for (int q = 0; q < Q; ++q) {
-            const V vx = __builtin_bit_cast(V, rx[q]), vd = __builtin_bit_cast(V, rd[q]);
+        for (int u = 0; u < U; ++u) {
+            float s1 = 0.f, s2 = 0.f;
 #pragma unroll
-            for (int e = 0; e < P; ++e) {
-                const float h = ((float)vx[e] - mean) * rstd, d = (float)vd[e], g = d * gamma[q][e];
-                // (columns behind the row: dy and gamma are zeros there, h is finite wherever the row's statistics are)
-                s1 += g;
-                s2 += (t + q * TPR) * P + e < p.D ? g * h : 0.f;
-                db[q][e] += d;
-                dg[q][e] += d * h;
+            for (int q = 0; q < Q; ++q) {
+                const V vx = __builtin_bit_cast(V, x.raw[u][q]), vd = __builtin_bit_cast(V, dy.raw[u][q]);
+#pragma unroll
+                for (int e = 0; e < P; ++e) {
+                    const float h = ((float)vx[e] - mean[u]) * rstd[u], d = (float)vd[e], g = d * gamma[q][e];
+                    // (columns behind the row: dy and gamma are zeros there)
+                    s1 += g;
+                    s2 += (t + q * TPR) * P + e < p.D ? g * h : 0.f;
+                    db[q][e] += d;
+                    dg[q][e] += d * h;
+                }
             }
+            s[2 * u] = s1;
+            s[2 * u + 1] = s2;
         }
-        row_sum(s1, s2);
-        if (!there || !p.out) continue;
-        s1 *= inv;
-        s2 *= inv;
-        T* const dx = static_cast<T*>(p.out) + r * p.ldo;
+        if (!p.out) continue;
+        row_sum(s);
 #pragma unroll
-        for (int q = 0; q < Q; ++q) {
-            const V vx = __builtin_bit_cast(V, rx[q]), vd = __builtin_bit_cast(V, rd[q]);
-            const int d = (t + q * TPR) * P, n = p.D - d;
-            V o;
+        for (int u = 0; u < U; ++u) {
+            const long long r = r0 + u * step;
+            if (r >= p.rows) break;
+            const float s1 = s[2 * u] * inv, s2 = s[2 * u + 1] * inv;
+            T* const dx = static_cast<T*>(p.out) + r * p.ldo;
 #pragma unroll
-            for (int e = 0; e < P; ++e) {
-                const float h = ((float)vx[e] - mean) * rstd;
-                o[e] = (T)(rstd * ((float)vd[e] * gamma[q][e] - s1 - h * s2));
+            for (int q = 0; q < Q; ++q) {
+                const V vx = __builtin_bit_cast(V, x.raw[u][q]), vd = __builtin_bit_cast(V, dy.raw[u][q]);
+                const int d = (t + q * TPR) * P, n = p.D - d;
+                V o;
+#pragma unroll
+                for (int e = 0; e < P; ++e) {
+                    const float h = ((float)vx[e] - mean[u]) * rstd[u];
+                    o[e] = (T)(rstd[u] * ((float)vd[e] * gamma[q][e] - s1 - h * s2));
+                }
+                if (n >= P) store16(dx + d, __builtin_bit_cast(uint4v, o));
+                else
+#pragma unroll
+                    for (int e = 0; e < P; ++e)
+                        if (e < n) dx[d + e] = o[e];
             }
-            if (n >= P) store16(dx + d, __builtin_bit_cast(uint4v, o));
-            else
-#pragma unroll
-                for (int e = 0; e < P; ++e)
-                    if (e < n) dx[d + e] = o[e];
         }
     }
     // the groups' sums of a column, in their order
@@ -217,17 +265,20 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(const NormArgs p) {
 #pragma unroll
                 for (int e = 0; e < P; ++e) columns[threadIdx.x * P + e] = sum[e];
                 __syncthreads();
-                if (group == 0)
-                    for (int g = 1; g < GROUPS; ++g)
-#pragma unroll
-                        for (int e = 0; e < P; ++e) sum[e] += columns[(g * TPR + t) * P + e];
-            }
-            if (group == 0)
+                // (a column of TPR * P at this q is one thread's: its groups' sums are TPR * P apart)
+                for (int c = threadIdx.x; c < TPR * P; c += THREADS) {
+                    float all = 0.f;
+                    for (int g = 0; g < GROUPS; ++g) all += columns[g * TPR * P + c];
+                    const int d = q * TPR * P + c;
+                    if (d < p.D) out[(size_t)blockIdx.x * p.D + d] = all;
+                }
+            } else {
 #pragma unroll
                 for (int e = 0; e < P; ++e) {
                     const int d = (t + q * TPR) * P + e;
                     if (d < p.D) out[(size_t)blockIdx.x * p.D + d] = sum[e];
                 }
+            }
         }
     }
 }
@@ -237,28 +288,26 @@ constexpr int kLong = 1024;
 template <int DT>
 __global__ __launch_bounds__(kLong) void norm_long_kernel(const NormArgs p) {
     typedef typename Store<DT>::T T;
-    __shared__ float room[2][2][16];
-    RowSum<kLong> row_sum{room};
+    __shared__ float room[2][1][16];
+    RowSum<kLong, 1> row_sum{room};
     for (long long r = blockIdx.x; r < p.rows; r += gridDim.x) {
         const T* const x = static_cast<const T*>(p.x) + r * p.ldx;
         T* const y = static_cast<T*>(p.out) + r * p.ldo;
-        float sum = 0.f, none = 0.f, v[8];
+        float sum[1] = {}, squares[1] = {}, v[8];
         for (int d = threadIdx.x * 8; d < p.D; d += kLong * 8) {
             load8<DT>(x + d, p.D - d, v);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum += v[e];
+            for (int e = 0; e < 8; ++e) sum[0] += v[e];
         }
-        row_sum(sum, none);
-        const float mean = sum / (float)p.D;
-        float squares = 0.f;
-        none = 0.f;
+        row_sum(sum);
+        const float mean = sum[0] / (float)p.D;
         for (int d = threadIdx.x * 8; d < p.D; d += kLong * 8) {
             load8<DT>(x + d, p.D - d, v);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) squares += d + e < p.D ? (v[e] - mean) * (v[e] - mean) : 0.f;
+            for (int e = 0; e < 8; ++e) squares[0] += d + e < p.D ? (v[e] - mean) * (v[e] - mean) : 0.f;
         }
-        row_sum(squares, none);
-        const float rstd = 1.f / sqrtf(squares / (float)p.D + p.eps);
+        row_sum(squares);
+        const float rstd = 1.f / sqrtf(squares[0] / (float)p.D + p.eps);
         if (threadIdx.x == 0) {
             if (p.mean) p.mean[r] = mean;
             if (p.rstd) p.rstd[r] = rstd;
@@ -278,13 +327,13 @@ template <int DT>
 __global__ __launch_bounds__(kLong) void norm_grad_long_kernel(const NormArgs p) {
     typedef typename Store<DT>::T T;
     __shared__ float room[2][2][16];
-    RowSum<kLong> row_sum{room};
+    RowSum<kLong, 2> row_sum{room};
     for (long long r = blockIdx.x; r < p.rows; r += gridDim.x) {
         const T* const x = static_cast<const T*>(p.x) + r * p.ldx;
         const T* const dy = static_cast<const T*>(p.dy) + r * p.lddy;
         T* const dx = static_cast<T*>(p.out) + r * p.ldo;
         const float mean = p.mean[r], rstd = p.rstd[r];
-        float s1 = 0.f, s2 = 0.f, vx[8], vd[8];
+        float s[2] = {}, vx[8], vd[8];
         for (int d = threadIdx.x * 8; d < p.D; d += kLong * 8) {
             const int n = p.D - d;
             load8<DT>(x + d, n, vx);
@@ -293,13 +342,12 @@ __global__ __launch_bounds__(kLong) void norm_grad_long_kernel(const NormArgs p)
             for (int e = 0; e < 8; ++e)
                 if (e < n) {
                     const float g = vd[e] * (p.gamma ? p.gamma[d + e] : 1.f);
-                    s1 += g;
-                    s2 += g * ((vx[e] - mean) * rstd);
+                    s[0] += g;
+                    s[1] += g * ((vx[e] - mean) * rstd);
                 }
         }
-        row_sum(s1, s2);
-        s1 /= (float)p.D;
-        s2 /= (float)p.D;
+        row_sum(s);
+        const float s1 = s[0] / (float)p.D, s2 = s[1] / (float)p.D;
         for (int d = threadIdx.x * 8; d < p.D; d += kLong * 8) {
             const int n = p.D - d;
             load8<DT>(x + d, n, vx);
@@ -350,22 +398,36 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(const NormArgs p, int
     }
 }
 
-// out[d] = sum of the parts [part][d]: 32 columns a workgroup, eight threads to a column, each a run of the parts
+// out[d] = sum of the parts [part][d]: 64 columns a workgroup, four a thread (one where D is no multiple of four), and 16 (4)
+// threads to a column, each with every 16th (4th) part, eight of them asked for at a time
+template <int C>
 __global__ __launch_bounds__(256) void norm_add_kernel(const float* dgamma_parts, const float* dbeta_parts, int parts, int D, float* dgamma,
                                                        float* dbeta) {
-    __shared__ float sums[8][32];
+    constexpr int W = 64 / C, S = 256 / W;
+    typedef float Vc __attribute__((ext_vector_type(C)));
+    __shared__ float sums[S][64];
     const float* const from = blockIdx.y ? dbeta_parts : dgamma_parts;
     float* const to = blockIdx.y ? dbeta : dgamma;
     if (!to) return;
-    const int c = threadIdx.x & 31, s = threadIdx.x >> 5, d = blockIdx.x * 32 + c, per = (parts + 7) / 8;
-    float sum = 0.f;
+    const int c = threadIdx.x % W * C, s = threadIdx.x / W, d = blockIdx.x * 64 + c;
+    float sum[C] = {};
     if (d < D)
-        for (int g = s * per; g < min(parts, (s + 1) * per); ++g) sum += from[(size_t)g * D + d];
-    sums[s][c] = sum;
+#pragma unroll 8
+        for (int g = s; g < parts; g += S) {
+            const Vc v = *reinterpret_cast<const Vc*>(from + (size_t)g * D + d);
+#pragma unroll
+            for (int e = 0; e < C; ++e)
+                if constexpr (C > 1) sum[e] += v[e];
+                else sum[e] += v[0];
+        }
+#pragma unroll
+    for (int e = 0; e < C; ++e) sums[s][c + e] = sum[e];
     __syncthreads();
-    if (s == 0 && d < D) {
-        for (int q = 1; q < 8; ++q) sum += sums[q][c];
-        to[d] = sum;
+    if (threadIdx.x < 64 && blockIdx.x * 64 + threadIdx.x < D) {
+        float all = 0.f;
+#pragma unroll
+        for (int q = 0; q < S; ++q) all += sums[q][threadIdx.x];
+        to[blockIdx.x * 64 + threadIdx.x] = all;
     }
 }
 
@@ -377,42 +439,58 @@ __global__ __launch_bounds__(256) void norm_zero_kernel(float* a, float* b, int 
     }
 }
 
-// How a row of `pieces` 16-byte pieces is spread: threads of a row, pieces of a thread, threads of a workgroup; tpr = 0: too long
-struct Spread { int tpr, q, threads; };
+// How a row of `pieces` 16-byte pieces is spread: threads of a row, pieces of a thread, rows at a time; tpr = 0: too long
+struct Spread { int tpr, q, u; };
 Spread spread(int pieces) {
-    if (pieces <= 8) return {8, 1, 256};
-    if (pieces <= 16) return {16, 1, 256};
-    if (pieces <= 32) return {32, 1, 256};
-    if (pieces <= 64) return {64, 1, 256};
-    if (pieces <= 128) return {64, 2, 256};
-    if (pieces <= 256) return {256, 1, 256};
-    if (pieces <= 512) return {256, 2, 256};
-    if (pieces <= 1024) return {512, 2, 512};
-    if (pieces <= 2048) return {1024, 2, 1024};
-    if (pieces <= 4096) return {1024, 4, 1024};
-    return {0, 0, kLong};
+    if (pieces <= 8) return {8, 1, 4};
+    if (pieces <= 16) return {16, 1, 4};
+    if (pieces <= 32) return {32, 1, 4};
+    if (pieces <= 64) return {64, 1, 4};
+    if (pieces <= 128) return {64, 2, 2};
+    if (pieces <= 256) return {256, 1, 2};
+    if (pieces <= 512) return {256, 2, 1};
+    if (pieces <= 1024) return {512, 2, 1};
+    if (pieces <= 2048) return {1024, 2, 1};
+    if (pieces <= 4096) return {1024, 4, 1};
+    return {0, 0, 1};
 }
+#define PCONV_SPREADS(X) X(8, 1, 4) X(16, 1, 4) X(32, 1, 4) X(64, 1, 4) X(64, 2, 2) X(256, 1, 2) X(256, 2, 1) X(512, 2, 1) X(1024, 2, 1) X(1024, 4, 1)
+// (the backward pass needs three times the registers)
+Spread grad_spread(int pieces) {
+    if (pieces <= 8) return {8, 1, 2};
+    if (pieces <= 16) return {16, 1, 2};
+    if (pieces <= 32) return {32, 1, 2};
+    if (pieces <= 64) return {64, 1, 2};
+    if (pieces <= 128) return {64, 2, 1};
+    if (pieces <= 256) return {256, 1, 1};
+    if (pieces <= 512) return {256, 2, 1};
+    if (pieces <= 1024) return {512, 2, 1};
+    if (pieces <= 2048) return {1024, 2, 1};
+    return {0, 0, 1};
+}
+#define PCONV_GRAD_SPREADS(X) X(8, 1, 2) X(16, 1, 2) X(32, 1, 2) X(64, 1, 2) X(64, 2, 1) X(256, 1, 1) X(256, 2, 1) X(512, 2, 1) X(1024, 2, 1)
 
+constexpr int forward_threads(int tpr) { return tpr > 256 ? tpr : 256; }
 int workgroups(const Spread& s, int rows) {
-    const int groups = s.tpr ? s.threads / s.tpr : 1;
+    const int threads = s.tpr ? forward_threads(s.tpr) : kLong, groups = s.tpr ? threads / s.tpr : 1;
     const long long wanted = ((long long)rows + groups - 1) / groups;
-    return (int)std::min<long long>(wanted, 256ll * (2048 / s.threads));
+    return (int)std::min<long long>(wanted, 256ll * (2048 / threads));
 }
+// (backward: one workgroup for a compute unit, so that there are few parts to add)
+constexpr int backward_threads(int tpr) { return tpr > 512 ? tpr : 512; }
 int grad_workgroups(const Spread& s, int rows) {
-    const int groups = s.tpr ? s.threads / s.tpr : 1;
-    const long long wanted = ((long long)rows + groups - 1) / groups;
-    return (int)std::min<long long>(wanted, 256ll * std::max(1, 1024 / s.threads));
+    const int groups = s.tpr ? backward_threads(s.tpr) / s.tpr : 1;
+    return (int)std::min<long long>(((long long)rows + groups - 1) / groups, 256);
 }
 int strips(int rows, int D) { return std::max(1, std::min({64, (int)((rows + 63ll) / 64), 512 / ((D + kSumCols - 1) / kSumCols) + 1})); }
-
-#define PCONV_SPREADS(X) X(8, 1, 256) X(16, 1, 256) X(32, 1, 256) X(64, 1, 256) X(64, 2, 256) X(256, 1, 256) X(256, 2, 256) X(512, 2, 512) X(1024, 2, 1024) X(1024, 4, 1024)
 
 template <int DT>
 int launch_norm(const NormArgs& a, hipStream_t st) {
     const Spread s = spread((a.D + Store<DT>::kPer - 1) / Store<DT>::kPer);
     const dim3 grid((unsigned)workgroups(s, a.rows));
-#define X(TPR, Q, THREADS) \
-    if (s.tpr == TPR && s.q == Q) hipLaunchKernelGGL((norm_kernel<DT, TPR, Q, THREADS>), grid, dim3(THREADS), 0, st, a);
+#define X(TPR, Q, U)              \
+    if (s.tpr == TPR && s.q == Q) \
+        hipLaunchKernelGGL((norm_kernel<DT, TPR, Q, U, forward_threads(TPR)>), grid, dim3(forward_threads(TPR)), 0, st, a);
     PCONV_SPREADS(X)
 #undef X
     if (!s.tpr) hipLaunchKernelGGL(norm_long_kernel<DT>, grid, dim3(kLong), 0, st, a);
@@ -422,21 +500,22 @@ int launch_norm(const NormArgs& a, hipStream_t st) {
 
 int grad_parts(int dtype, int rows, int D) {
     const int per = 16 / elem_bytes(dtype);
-    const Spread s = spread((D + per - 1) / per);
+    const Spread s = grad_spread((D + per - 1) / per);
     return s.tpr ? grad_workgroups(s, rows) : strips(rows, D);
 }
 
 template <int DT>
 int launch_norm_grad(NormArgs a, float* dgamma, float* dbeta, float* parts, hipStream_t st) {
-    const Spread s = spread((a.D + Store<DT>::kPer - 1) / Store<DT>::kPer);
+    const Spread s = grad_spread((a.D + Store<DT>::kPer - 1) / Store<DT>::kPer);
     const int n = grad_parts(DT, a.rows, a.D);
     // (a single part is the result)
     a.dgamma = dgamma ? n > 1 ? parts : dgamma : nullptr;
     a.dbeta = dbeta ? n > 1 ? parts + (size_t)n * a.D : dbeta : nullptr;
     const dim3 grid((unsigned)grad_workgroups(s, a.rows));
-#define X(TPR, Q, THREADS) \
-    if (s.tpr == TPR && s.q == Q) hipLaunchKernelGGL((norm_grad_kernel<DT, TPR, Q, THREADS>), grid, dim3(THREADS), 0, st, a);
-    PCONV_SPREADS(X)
+#define X(TPR, Q, U)              \
+    if (s.tpr == TPR && s.q == Q) \
+        hipLaunchKernelGGL((norm_grad_kernel<DT, TPR, Q, U, backward_threads(TPR)>), grid, dim3(backward_threads(TPR)), 0, st, a);
+    PCONV_GRAD_SPREADS(X)
 #undef X
     if (!s.tpr) {
         // (the columns first: dx may be written over x or dy)
@@ -448,7 +527,9 @@ int launch_norm_grad(NormArgs a, float* dgamma, float* dbeta, float* parts, hipS
     }
     PCONV_HIP(hipGetLastError());
     if (n > 1 && (dgamma || dbeta)) {
-        hipLaunchKernelGGL(norm_add_kernel, dim3((a.D + 31) / 32, 2), dim3(256), 0, st, a.dgamma, a.dbeta, n, a.D, dgamma, dbeta);
+        const dim3 blocks((a.D + 63) / 64, 2);
+        if (a.D % 4 == 0) hipLaunchKernelGGL(norm_add_kernel<4>, blocks, dim3(256), 0, st, a.dgamma, a.dbeta, n, a.D, dgamma, dbeta);
+        else hipLaunchKernelGGL(norm_add_kernel<1>, blocks, dim3(256), 0, st, a.dgamma, a.dbeta, n, a.D, dgamma, dbeta);
         PCONV_HIP(hipGetLastError());
     }
     return PCONV_OK;
