@@ -2,11 +2,12 @@
 // teacher's distribution over its k stored entries, the loss and the gradient of the logits.  Memory bounds it: the logits in
 // once, the gradient out once.
 //
-// One workgroup per row.  The row's logits stay in registers as they are stored, Q pieces of 16 bytes a thread (a row begins at any
-// element: pieces are those of memory, cut at the row's ends, so that every access is aligned): largest, sum of the
-// exponentials, gradient, all from one reading.  Longer rows are read again, with the running maximum and sum of a softmax
-// in the first pass.  The entries are held in LDS; after the row's w * T * q has been stored the entries' places are stored again
-// with their p taken off, by the first entry of each index (for all that share it).
+// One workgroup per row.  The row's logits are read once, Q pieces of 16 bytes a thread, and stay in registers, first as they are
+// stored, then as their exponentials: largest, sum of the exponentials, gradient.  (A row begins at any element: pieces are those
+// of memory, cut at the row's ends, so that every access is aligned.)  Longer rows are read again for the gradient, with the running
+// maximum and sum of a softmax in the first pass.  The entries are one wave's work, beside the reductions of the others; after the
+// row's w * T * q has been stored the entries' places are stored again with their p taken off, by the first entry of each index (for
+// all that share it).
 #include "pconv_dense_util.h"
 
 namespace pconv {
@@ -28,26 +29,25 @@ struct DistillArgs {
     float inv_t, t;
 };
 
-template <int THREADS, typename F>
-__device__ __forceinline__ float all_reduce(float v, float* room, F f) {
+template <typename F>
+__device__ __forceinline__ float wave_reduce(float v, F f) {
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) v = f(v, __shfl_xor(v, d, 64));
-    if constexpr (THREADS > 64) {
-        const int wave = threadIdx.x >> 6;
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) room[wave] = v;
-        __syncthreads();
-        v = room[0];
+    return v;
+}
+// `room`: a float of LDS per wave, read after the barrier in here
+template <int THREADS, typename F>
+__device__ __forceinline__ float all_reduce(float v, float* room, F f) {
+    v = wave_reduce(v, f);
+    if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = room[0];
 #pragma unroll
-        for (int w = 1; w < THREADS / 64; ++w) v = f(v, room[w]);
-    }
+    for (int w = 1; w < THREADS / 64; ++w) v = f(v, room[w]);
     return v;
 }
 __device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }     // (a NaN is passed over: the sum finds it)
 __device__ __forceinline__ float plus(float a, float b) { return a + b; }
-
-// exp(x) for x <= 0, NaN for NaN; exp(-inf) = 0
-__device__ __forceinline__ float exp_of(float x) { return __expf(x); }
 
 // Piece `q` of the row that begins `shift` elements into a 16-byte piece of memory: elements q * P - shift .. + P - 1
 template <int DT>
@@ -78,38 +78,31 @@ __device__ __forceinline__ void store_piece(typename Store<DT>::T* row, int at, 
     }
 }
 
+// Waves that a SIMD is to hold: two workgroups of 1024 threads a compute unit where 64 registers are enough
+[[maybe_unused]] constexpr int waves_per_simd(int threads, int pieces) { return pieces <= 4 ? 8 : threads / 256; }
+
 // Q = 0: the row is read again for the gradient
 template <int DT, int THREADS, int Q>
-__global__ __launch_bounds__(THREADS) void distill_kernel(const DistillArgs p) {
+__global__ __launch_bounds__(THREADS, waves_per_simd(THREADS, Q)) void distill_kernel(const DistillArgs p) {
     typedef typename Store<DT>::T T;
     typedef typename Store<DT>::V Vec;
     constexpr int P = Store<DT>::kPer;
-    __shared__ float room[16];
-    __shared__ int index[kMostEntries];
-    __shared__ float prob[kMostEntries];
-    __shared__ float at_index[kMostEntries];
-    const int t = threadIdx.x;
+    __shared__ float room[2][16];
+    __shared__ float teacher[2];                           // largest t / T or NaN, sum of the exponentials
+    extern __shared__ __align__(16) unsigned char entries[];
+    const int k4 = (p.k + 3) / 4 * 4;
+    int* const index = reinterpret_cast<int*>(entries);    // [k4], -1: not there
+    float* const prob = reinterpret_cast<float*>(index + k4);
+    float* const own = prob + k4;                          // the row's own logit at the index
+    const int t = threadIdx.x, lane = t & 63;
     const long long r = blockIdx.x;
     const T* const row = static_cast<const T*>(p.logits) + r * p.ldl;
     T* const out = static_cast<T*>(p.grad) + r * p.ldg;
     const int shift = (int)(reinterpret_cast<uintptr_t>(row) % 16) / (int)sizeof(T);
     const int pieces = (int)(((long long)p.V + shift + P - 1) / P);
     const float w = p.weight ? p.weight[r] : 1.f;
-
-    // the teacher's entries
-    float top = -__builtin_inff(), some = 0.f;
-    for (int j = t; j < p.k; j += THREADS) {
-        const int i = p.indices[r * p.k + j];
-        const bool there = i >= 0 && i < p.V;
-        const float v = there ? p.values[r * p.k + j] * p.inv_t : -__builtin_inff();
-        index[j] = there ? i : -1;
-        prob[j] = v;
-        top = fmaxf(top, v);
-        if (there && !(v == -__builtin_inff())) some = 1.f;
-    }
-    top = all_reduce<THREADS>(top, room, larger);
-    some = all_reduce<THREADS>(some, room, larger);
-    if (some == 0.f || w == 0.f) {                     // (the same for the whole workgroup)
+    // a row that is left out (the same for the whole workgroup)
+    auto leave_out = [&] {
         if (t == 0) {
             if (p.loss) p.loss[r] = 0.f;
             if (p.stats) p.stats[2 * r] = p.stats[2 * r + 1] = 0.f;
@@ -118,6 +111,9 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const DistillArgs p) {
             const float zero[P] = {};
             for (int q = t; q < pieces; q += THREADS) store_piece<DT>(out, q * P - shift, p.V, zero);
         }
+    };
+    if (w == 0.f) {
+        leave_out();
         return;
     }
     uint4v raw[Q ? Q : 1];
@@ -125,33 +121,45 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const DistillArgs p) {
 #pragma unroll
         for (int q = 0; q < Q; ++q) raw[q] = load_piece<DT>(row, (t + q * THREADS) * P - shift, p.V);
     }
-    float sum = 0.f;
-    for (int j = t; j < p.k; j += THREADS)
-        if (index[j] >= 0) sum += exp_of(prob[j] - top);
-    const float total = all_reduce<THREADS>(sum, room, plus);
-    const float log_total = logf(total);
 
-    // the softmax of the row
-    float largest, norm;
+    // the teacher's entries: the first wave's lanes, j = lane, lane + 64, ..
+    if (t < 64) {
+        float top = -__builtin_inff(), some = 0.f, sum = 0.f;
+        for (int j = lane; j < k4; j += 64) {
+            const int i = j < p.k ? p.indices[r * p.k + j] : -1;
+            const bool there = i >= 0 && i < p.V;
+            const float v = there ? p.values[r * p.k + j] * p.inv_t : -__builtin_inff();
+            index[j] = there ? i : -1;
+            prob[j] = v;
+            top = fmaxf(top, v);
+            if (there && !(v == -__builtin_inff())) some = 1.f;
+        }
+        top = wave_reduce(top, larger);
+        some = wave_reduce(some, larger);
+        for (int j = lane; j < k4; j += 64)
+            if (index[j] >= 0) sum += __expf(prob[j] - top);
+        sum = wave_reduce(sum, plus);
+        if (t == 0) {
+            teacher[0] = top;
+            teacher[1] = some == 0.f ? 0.f : sum;           // (a sum of 0: nothing is there; otherwise 1 or more, or NaN)
+        }
+    }
+
+    // the softmax of the row: largest, then the sum of u = exp((s - largest) / T)
+    const float c = p.inv_t * 1.44269504088896341f;
+    float u[Q ? Q : 1][P];
+    float largest, norm = 0.f, m = -__builtin_inff();
     if (p.given) {
         largest = p.given[2 * r];
         norm = p.given[2 * r + 1];
+        __syncthreads();
     } else {
-        float m = -__builtin_inff(), s = 0.f;
         if constexpr (Q > 0) {
 #pragma unroll
             for (int q = 0; q < Q; ++q) {
                 const Vec v = __builtin_bit_cast(Vec, raw[q]);
 #pragma unroll
                 for (int e = 0; e < P; ++e) m = fmaxf(m, (float)v[e]);
-            }
-            largest = all_reduce<THREADS>(m, room, larger);
-#pragma unroll
-            for (int q = 0; q < Q; ++q) {
-                const Vec v = __builtin_bit_cast(Vec, raw[q]);
-                const int at = (t + q * THREADS) * P - shift;
-#pragma unroll
-                for (int e = 0; e < P; ++e) s += at + e >= 0 && at + e < p.V ? exp_of(((float)v[e] - largest) * p.inv_t) : 0.f;
             }
         } else {
             for (int q = t; q < pieces; q += THREADS) {
@@ -160,80 +168,108 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const DistillArgs p) {
 #pragma unroll
                 for (int e = 0; e < P; ++e) high = fmaxf(high, (float)v[e]);
                 if (high > m) {
-                    s *= exp_of((m - high) * p.inv_t);
+                    norm *= __builtin_amdgcn_exp2f((m - high) * c);
                     m = high;
                 }
-                const int at = q * P - shift;
-                // (all of it -inf so far: nothing to add, unless there is a NaN)
+                // (-inf adds nothing, also where all has been -inf so far)
 #pragma unroll
                 for (int e = 0; e < P; ++e)
-                    if (at + e >= 0 && at + e < p.V && !((float)v[e] == -__builtin_inff())) s += exp_of(((float)v[e] - m) * p.inv_t);
+                    if (!((float)v[e] == -__builtin_inff())) norm += __builtin_amdgcn_exp2f(((float)v[e] - m) * c);
             }
-            largest = all_reduce<THREADS>(m, room, larger);
-            // (a thread whose logits were all -inf has a sum of 0; where every logit is, the sum is NaN)
-            if (m != largest) s *= exp_of((m - largest) * p.inv_t);
-            if (largest == -__builtin_inff()) s = __builtin_nanf("");
         }
-        norm = all_reduce<THREADS>(s, room, plus);
+        largest = all_reduce<THREADS>(m, room[0], larger);
+    }
+    const float top = teacher[0], total = teacher[1];
+    if (total == 0.f) {
+        leave_out();
+        return;
+    }
+    // the row's own logits at the entries, before any of the gradient is stored: grad may be logits
+    if (t < 64)
+        for (int j = lane; j < p.k; j += 64) own[j] = index[j] >= 0 ? (float)row[index[j]] : 0.f;
+    if constexpr (Q > 0) {
+        // (what lies outside the row is -inf: nothing, or NaN where the row is all -inf)
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            const Vec v = __builtin_bit_cast(Vec, raw[q]);
+#pragma unroll
+            for (int e = 0; e < P; ++e) u[q][e] = __builtin_amdgcn_exp2f(((float)v[e] - largest) * c);
+        }
+    }
+    if (!p.given) {
+        if constexpr (Q > 0) {
+#pragma unroll
+            for (int q = 0; q < Q; ++q)
+#pragma unroll
+                for (int e = 0; e < P; ++e) norm += u[q][e];
+        } else {
+            if (m != largest) norm *= __builtin_amdgcn_exp2f((m - largest) * c);
+            if (largest == -__builtin_inff()) norm = __builtin_nanf("");
+        }
+        norm = all_reduce<THREADS>(norm, room[1], plus);
         if (t == 0 && p.stats) {
             p.stats[2 * r] = largest;
             p.stats[2 * r + 1] = norm;
         }
+    } else {
+        __syncthreads();
     }
-    const float log_norm = logf(norm);
 
-    // loss, and what the entries' places will hold; an index that comes twice is looked for if the gradient is asked for
-    float loss = 0.f;
-    for (int j = t; j < p.k; j += THREADS) {
-        const int i = index[j];
-        if (i < 0) continue;
-        const float log_p = prob[j] - top - log_total, mine = exp_of(log_p);
-        const float z = ((float)row[i] - largest) * p.inv_t;
-        if (!(mine == 0.f)) loss += mine * (log_p - (z - log_norm));
-        at_index[j] = z;
-        prob[j] = mine;
+    // a total that is NaN makes the whole row NaN
+    const float scale = w * p.t, each = scale / norm * (total / total);
+    if (p.grad) {
+        if constexpr (Q > 0) {
+#pragma unroll
+            for (int q = 0; q < Q; ++q) {
+                const int at = (t + q * THREADS) * P - shift;
+                float g[P];
+#pragma unroll
+                for (int e = 0; e < P; ++e) g[e] = each * u[q][e];
+                if (at < p.V) store_piece<DT>(out, at, p.V, g);
+            }
+        } else {
+            for (int q = t; q < pieces; q += THREADS) {
+                const int at = q * P - shift;
+                const Vec v = __builtin_bit_cast(Vec, load_piece<DT>(row, at, p.V));
+                float g[P];
+#pragma unroll
+                for (int e = 0; e < P; ++e) g[e] = each * __builtin_amdgcn_exp2f(((float)v[e] - largest) * c);
+                store_piece<DT>(out, at, p.V, g);
+            }
+        }
     }
-    if (p.loss) {
-        loss = all_reduce<THREADS>(loss, room, plus);
-        if (t == 0) p.loss[r] = w * p.t * p.t * loss;
+    // the loss, and p in the place of t / T
+    if (t < 64) {
+        const float log_total = logf(total), log_norm = logf(norm);
+        float loss = 0.f;
+        for (int j = lane; j < p.k; j += 64) {
+            if (index[j] < 0) continue;
+            const float log_p = prob[j] - top - log_total, mine = __expf(log_p);
+            if (!(mine == 0.f)) loss += mine * (log_p - ((own[j] - largest) * p.inv_t - log_norm));
+            prob[j] = mine;
+        }
+        loss = wave_reduce(loss, plus);
+        if (p.loss && t == 0) p.loss[r] = w * p.t * p.t * loss;
     }
     if (!p.grad) return;
-
-    // a total that is NaN or +inf makes the whole row NaN
-    const float scale = w * p.t, each = scale / norm * (total / total);
-    __syncthreads();                                   // (every entry's logit has been read: grad may be logits)
-    if constexpr (Q > 0) {
-#pragma unroll
-        for (int q = 0; q < Q; ++q) {
-            const int at = (t + q * THREADS) * P - shift;
-            const Vec v = __builtin_bit_cast(Vec, raw[q]);
-            float g[P];
-#pragma unroll
-            for (int e = 0; e < P; ++e) g[e] = each * exp_of(((float)v[e] - largest) * p.inv_t);
-            if (at < p.V) store_piece<DT>(out, at, p.V, g);
-        }
-    } else {
-        for (int q = t; q < pieces; q += THREADS) {
-            const int at = q * P - shift;
-            const Vec v = __builtin_bit_cast(Vec, load_piece<DT>(row, at, p.V));
-            float g[P];
-#pragma unroll
-            for (int e = 0; e < P; ++e) g[e] = each * exp_of(((float)v[e] - largest) * p.inv_t);
-            store_piece<DT>(out, at, p.V, g);
-        }
-    }
     __syncthreads();
     for (int j = t; j < p.k; j += THREADS) {
         const int i = index[j];
         if (i < 0) continue;
         float mine = prob[j];
+        int alike = 0;
+        for (int o = 0; o < k4; o += 4) {
+            const int4 four = *reinterpret_cast<const int4*>(index + o);
+            alike += (four.x == i) + (four.y == i) + (four.z == i) + (four.w == i);
+        }
         bool first = true;
-        for (int o = 0; o < p.k; ++o)
-            if (o != j && index[o] == i) {
-                if (o < j) first = false;
-                else mine += prob[o];
-            }
-        if (first) out[i] = (T)(each * exp_of(at_index[j]) - scale * mine);
+        if (alike > 1)
+            for (int o = 0; o < p.k; ++o)
+                if (o != j && index[o] == i) {
+                    if (o < j) first = false;
+                    else mine += prob[o];
+                }
+        if (first) out[i] = (T)(each * __builtin_amdgcn_exp2f((own[j] - largest) * c) - scale * mine);
     }
 }
 
@@ -241,14 +277,15 @@ template <int DT>
 int launch_distill(const DistillArgs& a, int R, hipStream_t st) {
     constexpr int P = Store<DT>::kPer;
     const int pieces = a.V / P + 2;                    // (of a row that begins anywhere)
+    const size_t lds = 3 * (size_t)((a.k + 3) / 4 * 4) * 4;
 #define PCONV_ROWS(THREADS, Q)                                                                                   \
     if (!done && pieces <= THREADS * Q) {                                                                        \
-        hipLaunchKernelGGL((distill_kernel<DT, THREADS, Q>), dim3((unsigned)R), dim3(THREADS), 0, st, a);        \
+        hipLaunchKernelGGL((distill_kernel<DT, THREADS, Q>), dim3((unsigned)R), dim3(THREADS), lds, st, a);      \
         done = true;                                                                                             \
     }
     bool done = false;
     PCONV_ROWS(64, 2) PCONV_ROWS(256, 2) PCONV_ROWS(256, 4) PCONV_ROWS(1024, 2) PCONV_ROWS(1024, 4) PCONV_ROWS(1024, 8)
-    if (!done) hipLaunchKernelGGL((distill_kernel<DT, 1024, 0>), dim3((unsigned)R), dim3(1024), 0, st, a);
+    if (!done) hipLaunchKernelGGL((distill_kernel<DT, 1024, 0>), dim3((unsigned)R), dim3(1024), lds, st, a);
 #undef PCONV_ROWS
     PCONV_HIP(hipGetLastError());
     return PCONV_OK;
