@@ -35,7 +35,7 @@ struct Product {
 
 struct TileShape { int i, j, threads; };
 constexpr int kTiles = 3;
-constexpr TileShape kTileShapes[kTiles] = {{256, 256, 512}, {128, 128, 256}, {64, 64, 256}};
+constexpr TileShape kTileShapes[kTiles] = {{256, 256, 256}, {128, 128, 256}, {64, 64, 256}};
 constexpr int kStageBytes = 128;            // of c per stage, of one row
 
 int launch_product_f32(const Product& p, void* stream);

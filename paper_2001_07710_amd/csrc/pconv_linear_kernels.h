@@ -15,6 +15,9 @@
 //
 // The matrix instructions get B as their rows and A as their columns: a lane of the result then holds four consecutive j of one i.
 // They leave through a window of LDS that belongs to the wave, 32 i at a time, so that eight lanes store one 128-byte line.
+#include <type_traits>
+#include <utility>
+
 #include "pconv_dense_util.h"
 #include "pconv_linear.h"
 
@@ -22,27 +25,42 @@ namespace pconv {
 namespace {
 
 typedef __attribute__((address_space(3))) void* lds_ptr;
+typedef __attribute__((address_space(3))) unsigned char* lds_bytes;
 typedef __attribute__((address_space(3))) short4v* lds_short4;
+typedef const __attribute__((address_space(3))) uint4v* lds_uint4;
+typedef const __attribute__((address_space(3))) float* lds_float;
 
 constexpr int DT = PCONV_LINEAR_DT;
 typedef Store<DT>::T T;
 constexpr int ES = (int)sizeof(T);
 constexpr int PER = 16 / ES;                 // elements of a piece
 constexpr int BK = kStageBytes / ES;         // elements of c in a stage
-constexpr int KS = 4;                        // steps of a stage: two pieces of c each
+constexpr int KS = kStageBytes / 64;         // steps of a stage: four pieces of c each
 
-// acc += rows x columns over two pieces of c: lanes 0-31 hold the first, lanes 32-63 the second, of row / column lane % 32
-__device__ __forceinline__ float16v mma(uint4v a, uint4v b, float16v acc) {
+// acc += rows x columns over four pieces of c: lanes 16 g .. 16 g + 15 hold piece g of row / column lane % 16.  (16 x 16 x 32 and not
+// 32 x 32 x 16: the same rate by the clock, but half the traffic of accumulators, and the chip's power is what bounds large products:
+// 2195 against 2010 TFLOP/s on random operands in registers, bf16.)
+__device__ __forceinline__ float4v mma(uint4v a, uint4v b, float4v acc) {
     if constexpr (DT == PCONV_F16)
-        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), acc, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), acc, 0, 0, 0);
     else if constexpr (DT == PCONV_BF16)
-        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
     else {
         const float4v x = __builtin_bit_cast(float4v, a), y = __builtin_bit_cast(float4v, b);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(x[q], y[q], acc, 0, 0, 0);
+        for (int q = 0; q < 4; ++q) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(x[q], y[q], acc, 0, 0, 0);
         return acc;
     }
+}
+
+// f(0), f(1), .. f(N - 1) with constants (the unroller gives up on bodies of this size)
+template <typename F, int... I>
+__device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, F f) {
+    (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void each(F f) {
+    each_of(std::make_integer_sequence<int, N>{}, f);
 }
 
 struct Args {
@@ -119,32 +137,33 @@ struct Operand {
     static_assert(THREADS % kLinePieces == 0 && kBytes % (16 * THREADS) == 0, "a thread's pieces lie under each other");
     static __device__ __forceinline__ int swizzle(int line) {
         if constexpr (!ROWS) return (line >> 1) & 7;
-        // four lines of 64 bytes are read at once: they go to different quarters of 256 bytes
-        else return kLinePieces >= 16 ? (line & 3) * 4 : ((line >> 1) & 1) * 4;
+        else if constexpr (ES == 4) return ((line >> 2) & 3) * 4;              // lines 4 g + q: to different 64 bytes of 256
+        // lines 8 g + 4 q + 0..3, 32 bytes of each: to different 32 bytes of 256 for two g (lines of 128 bytes lie so by halves)
+        else return kLinePieces >= 16 ? ((line & 3) | ((line >> 1) & 4)) * 2 : (((line >> 1) & 1) | ((line >> 2) & 2)) * 2;
     }
-    static constexpr int kPeriod = ROWS ? 4 : 16;
-    static_assert(kLinesPer % kPeriod == 0 || kPieces == 1 || kLinesPer < kPeriod, "");
+    static constexpr int kReads = ROWS ? ES == 2 ? 2 : 4 : 1;             // LDS reads of one operand
+    static constexpr int kPeriod = 16;                                    // of the swizzle, in lines
+    static constexpr int kVariants = kLinesPer % kPeriod == 0 ? 1 : kPeriod / kLinesPer;     // of a thread's piece, by q
+    static_assert(kLinesPer % kPeriod == 0 || kPeriod % kLinesPer == 0, "");
 
     // line and piece of the matrix that thread t's piece q holds
     static __device__ __forceinline__ void where(int t, int q, int* line, int* piece) {
         *line = t / kLinePieces + q * kLinesPer;
         *piece = (t % kLinePieces) ^ swizzle(*line);
     }
-    // operand registers of 32-row block `blk` at step s
-    static __device__ __forceinline__ uint4v read(const unsigned char* lds, int blk, int s, int lane) {
-        const int r = lane & 31, h = lane >> 5;
+    // operand registers of 16-row block `blk` at step s
+    static __device__ __forceinline__ uint4v read(lds_bytes lds, int blk, int s, int lane) {
+        const int r = lane & 15, g = lane >> 4;
         if constexpr (!ROWS) {
-            const int row = blk * 32 + r;
-            return *reinterpret_cast<const uint4v*>(lds + row * kStageBytes + (((2 * s + h) ^ swizzle(row)) * 16));
+            const int row = blk * 16 + r;
+            return *(lds_uint4)(lds + row * kStageBytes + (((4 * s + g) ^ swizzle(row)) * 16));
         } else if constexpr (ES == 2) {
             uint4v v;
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
-                const int u = lane & 15, c = 16 * s + 8 * h + 4 * q + (u >> 2);
-                const int at = (blk * 32 + 16 * ((lane >> 4) & 1) + 4 * (u & 3)) * 2;
-                const unsigned char* p = lds + c * kLineBytes + (((at >> 4) ^ swizzle(c)) << 4) + (at & 15);
-                const short4v w = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4)p);
-                const uint2v d = __builtin_bit_cast(uint2v, w);
+                const int c = 32 * s + 8 * g + 4 * q + (r >> 2), at = (blk * 16 + 4 * (r & 3)) * 2;
+                const lds_bytes p = lds + c * kLineBytes + (((at >> 4) ^ swizzle(c)) << 4) + (at & 15);
+                const uint2v d = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4)p));
                 if (q) { v.z = d.x; v.w = d.y; } else { v.x = d.x; v.y = d.y; }
             }
             return v;
@@ -152,8 +171,8 @@ struct Operand {
             float4v v;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int c = 8 * s + 4 * h + q, at = (blk * 32 + r) * 4;
-                v[q] = *reinterpret_cast<const float*>(lds + c * kLineBytes + (((at >> 4) ^ swizzle(c)) << 4) + (at & 15));
+                const int c = 16 * s + 4 * g + q, at = (blk * 16 + r) * 4;
+                v[q] = *(lds_float)(lds + c * kLineBytes + (((at >> 4) ^ swizzle(c)) << 4) + (at & 15));
             }
             return __builtin_bit_cast(uint4v, v);
         }
@@ -162,7 +181,7 @@ struct Operand {
 
 template <bool AR, bool BR, int WI, int WJ, int AF, int BF, bool DIRECT>
 __global__ __launch_bounds__(WI * WJ * 64) void product_kernel(const Args p) {
-    constexpr int THREADS = WI * WJ * 64, TI = 32 * AF * WI, TJ = 32 * BF * WJ;
+    constexpr int THREADS = WI * WJ * 64, TI = 16 * AF * WI, TJ = 16 * BF * WJ;
     typedef Operand<AR, TI, THREADS> OA;
     typedef Operand<BR, TJ, THREADS> OB;
     constexpr int STAGE = OA::kBytes + OB::kBytes;
@@ -190,49 +209,68 @@ __global__ __launch_bounds__(WI * WJ * 64) void product_kernel(const Args p) {
     const unsigned long long b_step = BR ? (unsigned long long)p.ldb * BK : kStageBytes;
     int c_left = c1 - c0;
 
-    float16v acc[AF][BF];
+    float4v acc[AF][BF];
 #pragma unroll
     for (int a = 0; a < AF; ++a)
 #pragma unroll
-        for (int b = 0; b < BF; ++b)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[a][b][r] = 0.f;
+        for (int b = 0; b < BF; ++b) acc[a][b] = float4v{0.f, 0.f, 0.f, 0.f};
 
-    uint4v ra[DIRECT ? 1 : OA::kPieces], rb[DIRECT ? 1 : OB::kPieces];
-    // one operand's stage: into LDS (DIRECT), or into registers
-    auto ask = [&](auto tag, const unsigned char* at, unsigned long long left, long long ld, int rows, unsigned char* to, uint4v* regs) {
-        typedef decltype(tag) O;
-        constexpr bool R = O::kRows;
-        if constexpr (DIRECT) {
-            const auto rsrc = make_rsrc(at, (uint32_t)min(left, 0x7FFFFFFFull));
-            int line, piece;
-            O::where(t, 0, &line, &piece);
-            unsigned off = (unsigned)(line * ld) + piece * 16;
-            if (!R && piece * PER >= c_left) off = kInvalid;
+    // DIRECT: the stage that is being asked for, a piece at a time
+    constexpr int PIECES = OA::kPieces + OB::kPieces;
+    __amdgpu_buffer_rsrc_t rsrc_a, rsrc_b;
+    unsigned off_a[OA::kVariants], off_b[OB::kVariants];
+    int to_stage = 0;
+    auto begin_stage = [&](int buf) {
+        auto offsets = [&](auto tag, long long ld, unsigned* off) {
+            typedef decltype(tag) O;
 #pragma unroll
-            for (int q = 0; q < O::kPieces; ++q)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr)(to + (q * THREADS + wave * 64) * 16), 16,
-                                                         (int)(off + (unsigned)(q * O::kLinesPer * ld)), 0, 0, 0);
-        } else {
-#pragma unroll
-            for (int q = 0; q < O::kPieces; ++q) {
+            for (int v = 0; v < O::kVariants; ++v) {
                 int line, piece;
-                O::where(t, q, &line, &piece);
-                const int lines = R ? c_left : rows, along = (R ? rows : c_left) - piece * PER;
-                regs[q] = uint4v{0, 0, 0, 0};
-                if (line < lines && along > 0)
-                    regs[q] = load_part<DT>(reinterpret_cast<const T*>(at + line * ld) + piece * PER, along);
+                O::where(t, v, &line, &piece);
+                off[v] = !O::kRows && piece * PER >= c_left ? kInvalid : (unsigned)(line * ld) + piece * 16;
             }
-        }
-    };
-    auto ask_stage = [&](int buf) {
-        unsigned char* const to = lds + buf * STAGE;
-        ask(OA{}, pa, a_left, p.lda, p.I - i0, to, ra);
-        ask(OB{}, pb, b_left, p.ldb, p.J - j0, to + OA::kBytes, rb);
+        };
+        // (behind the last stage nothing is there: zeros, which nobody reads)
+        rsrc_a = make_rsrc(pa, c_left > 0 ? (uint32_t)min(a_left, 0x7FFFFFFFull) : 0);
+        rsrc_b = make_rsrc(pb, c_left > 0 ? (uint32_t)min(b_left, 0x7FFFFFFFull) : 0);
+        offsets(OA{}, p.lda, off_a);
+        offsets(OB{}, p.ldb, off_b);
+        to_stage = buf * STAGE + wave * 1024;
         pa += a_step;
         pb += b_step;
         a_left -= a_step;
         b_left -= b_step;
+        c_left -= BK;
+    };
+    auto ask_piece = [&](lds_bytes into, int q) {
+        if (q < OA::kPieces) {
+            const int v = q % OA::kVariants;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_a, (lds_ptr)(into + to_stage + q * THREADS * 16), 16,
+                                                     (int)(off_a[v] + (unsigned)((q - v) * OA::kLinesPer * p.lda)), 0, 0, 0);
+        } else {
+            const int o = q - OA::kPieces, v = o % OB::kVariants;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_b, (lds_ptr)(into + to_stage + OA::kBytes + o * THREADS * 16), 16,
+                                                     (int)(off_b[v] + (unsigned)((o - v) * OB::kLinesPer * p.ldb)), 0, 0, 0);
+        }
+    };
+    // through registers: a stage's pieces
+    uint4v ra[DIRECT ? 1 : OA::kPieces], rb[DIRECT ? 1 : OB::kPieces];
+    auto fetch = [&](auto tag, const unsigned char* at, long long ld, int rows, uint4v* regs) {
+        typedef decltype(tag) O;
+#pragma unroll
+        for (int q = 0; q < O::kPieces; ++q) {
+            int line, piece;
+            O::where(t, q, &line, &piece);
+            const int lines = O::kRows ? c_left : rows, along = (O::kRows ? rows : c_left) - piece * PER;
+            regs[q] = uint4v{0, 0, 0, 0};
+            if (line < lines && along > 0) regs[q] = load_part<DT>(reinterpret_cast<const T*>(at + line * ld) + piece * PER, along);
+        }
+    };
+    auto fetch_stage = [&] {
+        fetch(OA{}, pa, p.lda, p.I - i0, ra);
+        fetch(OB{}, pb, p.ldb, p.J - j0, rb);
+        pa += a_step;
+        pb += b_step;
         c_left -= BK;
     };
     auto put_stage = [&](int buf) {
@@ -245,55 +283,104 @@ __global__ __launch_bounds__(WI * WJ * 64) void product_kernel(const Args p) {
         }
     };
 
-    ask_stage(0);
-    put_stage(0);
-    for (int s = 0; s < stages; ++s) {
-        const int buf = s & 1;
-        __builtin_amdgcn_s_waitcnt(0x0F70);    // vmcnt(0): this wave's pieces of stage s are in LDS
-        __syncthreads();                       // so are the other waves', and none reads the other half any more
-        if (s + 1 < stages) ask_stage(buf ^ 1);
-        const unsigned char *la = lds + buf * STAGE, *lb = la + OA::kBytes;
+    typedef uint4v FragA[AF];
+    typedef uint4v FragB[BF];
+    auto read_one = [&](lds_bytes from, int buf, int k, int q, FragA& fa, FragB& fb) {
+        const lds_bytes la = from + buf * STAGE, lb = la + OA::kBytes;
+        if (q < BF) fb[q] = OB::read(lb, wj * BF + q, k, lane);
+        else fa[q - BF] = OA::read(la, wi * AF + q - BF, k, lane);
+    };
+    if constexpr (DIRECT) {
+        // A step's operands are read while the step before is multiplied, across stages too: the barrier that publishes stage
+        // s + 1 stands in front of stage s's last step, whose operands are in registers by then, so that stage s + 2 can be asked
+        // for into the same half: a piece at a time between the MFMAs of that step (asked for together they stand in the way of
+        // every wave's next instructions until the memory pipeline has taken them).
+        static_assert(KS == 2, "");
+        constexpr int MFMAS = AF * BF, READS = AF + BF;
+        // (two pointers to the stages, said not to alias, or the compiler waits for every piece that is under way in front of each
+        // ds_read_b64_tr_b16: what keeps them apart are the waits and barriers below)
+        auto main_loop = [&](const lds_bytes __restrict into, const lds_bytes __restrict from) {
+            FragA fa[2];
+            FragB fb[2];
+            auto step = [&](auto kk, int buf) {
+                constexpr int k = kk;
+                each<MFMAS>([&](auto mm) {
+                    constexpr int m = mm;
+                    // (behind the last stage: what is there, and not used)
+                    each<READS>([&](auto q) {
+                        if constexpr (q * MFMAS / READS == m) read_one(from, k == 0 ? buf : buf ^ 1, k ^ 1, q, fa[k ^ 1], fb[k ^ 1]);
+                    });
+                    if constexpr (k == 1)
+                        each<PIECES>([&](auto q) {
+                            if constexpr (q * MFMAS / PIECES == m) ask_piece(into, q);
+                        });
+                    acc[m / BF][m % BF] = mma(fb[k][m % BF], fa[k][m / BF], acc[m / BF][m % BF]);
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+            };
+            each<2>([&](auto s) {
+                begin_stage(s);
+                each<PIECES>([&](auto q) { ask_piece(into, q); });
+            });
+            __builtin_amdgcn_s_waitcnt(0x0F70 | (PIECES & 15) | (PIECES >> 4) << 14);      // vmcnt: all but the pieces of stage 1
+            __syncthreads();
+            each<READS>([&](auto q) { read_one(from, 0, 0, q, fa[0], fb[0]); });
+            for (int s = 0; s < stages; ++s) {
+                step(std::integral_constant<int, 0>{}, s & 1);
+                __builtin_amdgcn_s_waitcnt(0x0F70);        // vmcnt(0): this wave's pieces of stage s + 1 are in LDS
+                __syncthreads();                           // so are the other waves', and all have read stage s
+                begin_stage(s & 1);
+                __builtin_amdgcn_sched_barrier(0);
+                step(std::integral_constant<int, 1>{}, s & 1);
+            }
+        };
+        lds_bytes into = (lds_bytes)lds, from = into;
+        asm("" : "+s"(into), "+s"(from));              // (or it knows that they are the same)
+        main_loop(into, from);
+        __builtin_amdgcn_s_waitcnt(0x0F70);
+    } else {
+        fetch_stage();
+        put_stage(0);
+        for (int s = 0; s < stages; ++s) {
+            const int buf = s & 1;
+            __syncthreads();                   // stage s is in LDS for every wave, and no wave reads the other half any more
+            if (s + 1 < stages) fetch_stage();
 #pragma unroll
-        for (int k = 0; k < KS; ++k) {
-            uint4v fa[AF], fb[BF];
+            for (int k = 0; k < KS; ++k) {
+                FragA fa;
+                FragB fb;
 #pragma unroll
-            for (int b = 0; b < BF; ++b) fb[b] = OB::read(lb, wj * BF + b, k, lane);
+                for (int q = 0; q < AF + BF; ++q) read_one((lds_bytes)lds, buf, k, q, fa, fb);
 #pragma unroll
-            for (int a = 0; a < AF; ++a) fa[a] = OA::read(la, wi * AF + a, k, lane);
-#pragma unroll
-            for (int a = 0; a < AF; ++a)
-#pragma unroll
-                for (int b = 0; b < BF; ++b) acc[a][b] = mma(fb[b], fa[a], acc[a][b]);
+                for (int m = 0; m < AF * BF; ++m) acc[m / BF][m % BF] = mma(fb[m % BF], fa[m / BF], acc[m / BF][m % BF]);
+            }
+            if (s + 1 < stages) put_stage(buf ^ 1);
         }
-        if (s + 1 < stages) put_stage(buf ^ 1);
     }
     __syncthreads();
 
-    // results: a window of 32 i x 32 BF j floats for each wave, a pitch that spreads the rows over the banks
-    constexpr int PITCH = (32 * BF + 4) * 4, ROW_LANES = 4 * BF, ROWS_AT_ONCE = 64 / ROW_LANES;
-    static_assert(WI * WJ * 32 * PITCH <= 2 * STAGE, "the windows fit the stages");
-    unsigned char* const win = lds + wave * 32 * PITCH;
+    // results: a window of 16 i x 16 BF j floats for each wave, a pitch that spreads the rows over the banks
+    constexpr int PITCH = (16 * BF + 4) * 4, ROW_LANES = 2 * BF, ROWS_AT_ONCE = 64 / ROW_LANES;
+    static_assert(WI * WJ * 16 * PITCH <= 2 * STAGE && 16 % ROWS_AT_ONCE == 0, "the windows fit the stages");
+    unsigned char* const win = lds + wave * 16 * PITCH;
     Finish f = p.f;
     if (p.parts) {
         f.kind = kFloat;
         f.out = p.parts + (unsigned long long)split * p.I * p.J;
         f.ld_out = p.J;
     }
-    const int j = j0 + wj * 32 * BF + (lane % ROW_LANES) * 8, n = p.J - j;
+    const int j = j0 + wj * 16 * BF + (lane % ROW_LANES) * 8, n = p.J - j;
     float bias[8];
     bias8(f, j, n, bias);
-    auto put_block = [&](const float16v (&block)[BF]) {
+    auto put_block = [&](const float4v (&block)[BF]) {
 #pragma unroll
         for (int b = 0; b < BF; ++b)
-#pragma unroll
-            for (int g = 0; g < 4; ++g)
-                *reinterpret_cast<float4v*>(win + (lane & 31) * PITCH + (b * 32 + g * 8 + (lane >> 5) * 4) * 4) =
-                    float4v{block[b][4 * g], block[b][4 * g + 1], block[b][4 * g + 2], block[b][4 * g + 3]};
+            *reinterpret_cast<float4v*>(win + (lane & 15) * PITCH + (b * 16 + (lane >> 4) * 4) * 4) = block[b];
     };
-    constexpr int TIMES = 32 / ROWS_AT_ONCE;
+    constexpr int TIMES = 16 / ROWS_AT_ONCE;
 #pragma unroll 1
     for (int a = 0; a < AF; ++a) {
-        const int i = i0 + (wi * AF + a) * 32 + lane / ROW_LANES;
+        const int i = i0 + (wi * AF + a) * 16 + lane / ROW_LANES;
         Beside beside[TIMES];
 #pragma unroll
         for (int r = 0; r < TIMES; ++r)
@@ -338,19 +425,6 @@ __global__ __launch_bounds__(256) void add_parts_kernel(const float* parts, int 
 // workgroup owns 16 rows of w; its waves take turns along k (a wave's 64 lanes: 16 rows x 4 pieces), and their sums meet in LDS
 // in the order of the waves.  v_mfma_f32_16x16x32: rows of the result are rows of w, its columns rows of x.
 constexpr int kFewWaves = 8;
-__device__ __forceinline__ float4v mma16(uint4v a, uint4v b, float4v acc) {
-    if constexpr (DT == PCONV_F16)
-        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), acc, 0, 0, 0);
-    else if constexpr (DT == PCONV_BF16)
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
-    else {
-        const float4v x = __builtin_bit_cast(float4v, a), y = __builtin_bit_cast(float4v, b);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(x[q], y[q], acc, 0, 0, 0);
-        return acc;
-    }
-}
-
 __global__ __launch_bounds__(kFewWaves * 64) void few_rows_kernel(const Args p) {
     __shared__ __align__(16) float sums[kFewWaves][16][20];
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -373,7 +447,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_rows_kernel(const Args p) 
             if (has_x) x[u] = load16(px + c + u * STEP + piece * PER);
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u) acc = mma16(w[u], x[u], acc);
+        for (int u = 0; u < U; ++u) acc = mma(w[u], x[u], acc);
     }
     if (c < c1) {
 #pragma unroll
@@ -382,7 +456,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_rows_kernel(const Args p) 
             const uint4v w = load_part<DT>(pw + at, c1 - at);
             uint4v x = {0, 0, 0, 0};
             if (has_x) x = load_part<DT>(px + at, c1 - at);
-            acc = mma16(w, x, acc);
+            acc = mma(w, x, acc);
         }
     }
     *reinterpret_cast<float4v*>(&sums[wave][r][4 * piece]) = acc;            // [row of x][row of w]
@@ -439,7 +513,7 @@ int add_parts(const Product& p, hipStream_t st) {
 
 template <bool AR, bool BR, int WI, int WJ, int AF, int BF>
 int launch_tile(const Product& p, bool direct, hipStream_t st) {
-    constexpr int TI = 32 * AF * WI, TJ = 32 * BF * WJ;
+    constexpr int TI = 16 * AF * WI, TJ = 16 * BF * WJ;
     const Args a = make_args(p, TI, TJ);
     const size_t lds = 2 * (size_t)(TI + TJ) * kStageBytes;
     const unsigned long long grid = (unsigned long long)a.tiles_i * a.tiles_j * p.splits;
@@ -465,9 +539,9 @@ int launch_form(const Product& p, hipStream_t st) {
     };
     const bool direct = fits(p.a, p.lda, AR) && fits(p.b, p.ldb, BR);
     switch (p.tile) {
-        case 0: return launch_tile<AR, BR, 2, 4, 4, 2>(p, direct, st);
-        case 1: return launch_tile<AR, BR, 2, 2, 2, 2>(p, direct, st);
-        default: return launch_tile<AR, BR, 2, 2, 1, 1>(p, direct, st);
+        case 0: return launch_tile<AR, BR, 2, 2, 8, 8>(p, direct, st);
+        case 1: return launch_tile<AR, BR, 2, 2, 4, 4>(p, direct, st);
+        default: return launch_tile<AR, BR, 2, 2, 2, 2>(p, direct, st);
     }
 }
 
