@@ -79,6 +79,10 @@ struct Eight {
 #pragma unroll
         for (int h = 0; h < 8 / P; ++h) raw[h] = load_part<DT>(p + h * P, n - h * P);
     }
+    __device__ __forceinline__ void load_whole(const typename Store<DT>::T* p) {
+#pragma unroll
+        for (int h = 0; h < 8 / P; ++h) raw[h] = load16(p + h * P);
+    }
     __device__ __forceinline__ void get(float out[8]) const {
 #pragma unroll
         for (int h = 0; h < 8 / P; ++h) {
@@ -141,10 +145,12 @@ __device__ __forceinline__ float silu_slope(float z) {
     return s * (1.f + t * (1.f - s));
 }
 
-// v[q] = curve(v[q]), or v[q] *= slope(z[q])
-__device__ __forceinline__ void activate8(float v[8], int act) {
-#define PCONV_EACH(F)                                   \
-    _Pragma("unroll") for (int q = 0; q < 8; ++q) v[q] = F(v[q]); \
+// v = curve(v), or v *= slope(z), for R times eight values
+template <int R>
+__device__ __forceinline__ void activate8(float v[R][8], int act) {
+#define PCONV_EACH(F)                                         \
+    _Pragma("unroll") for (int r = 0; r < R; ++r)             \
+        _Pragma("unroll") for (int q = 0; q < 8; ++q) v[r][q] = F(v[r][q]); \
     break
     switch (act) {
         case PCONV_ACT_RELU: PCONV_EACH(relu);
@@ -155,9 +161,11 @@ __device__ __forceinline__ void activate8(float v[8], int act) {
     }
 #undef PCONV_EACH
 }
-__device__ __forceinline__ void times_slope8(float v[8], const float z[8], int act) {
-#define PCONV_EACH(F)                                   \
-    _Pragma("unroll") for (int q = 0; q < 8; ++q) v[q] *= F(z[q]); \
+template <int R>
+__device__ __forceinline__ void times_slope8(float v[R][8], const float z[R][8], int act) {
+#define PCONV_EACH(F)                                         \
+    _Pragma("unroll") for (int r = 0; r < R; ++r)             \
+        _Pragma("unroll") for (int q = 0; q < 8; ++q) v[r][q] *= F(z[r][q]); \
     break
     switch (act) {
         case PCONV_ACT_RELU: PCONV_EACH(relu_slope);

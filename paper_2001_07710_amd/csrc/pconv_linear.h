@@ -33,6 +33,7 @@ struct Product {
     float* parts;               // splits > 1: [splits][I][J] partial sums
 };
 
+constexpr int kComputeUnits = 256;          // of an MI355X: plans and workspaces are the same whatever device is current
 struct TileShape { int i, j, threads; };
 constexpr int kTiles = 3;
 constexpr TileShape kTileShapes[kTiles] = {{256, 256, 256}, {128, 128, 256}, {64, 64, 256}};

@@ -7,7 +7,6 @@ namespace pconv {
 namespace {
 
 constexpr int kMostRows = 1 << 30;          // (the kernels count rows, and stages of a product over rows, in 32 bits)
-constexpr int kComputeUnits = 256;          // of an MI355X: plans and workspaces are the same whatever device is current
 
 struct Plan {
     int tile = 0;                           // kTiles: the kernel for few rows
@@ -134,11 +133,11 @@ __global__ __launch_bounds__(256) void activation_grad_kernel(const typename Sto
     const unsigned long long at = (unsigned long long)blockIdx.x * 256 + threadIdx.x, i = at / per_row;
     if (i >= (unsigned long long)M) return;
     const int j = (int)(at % per_row) * 8, n = N - j;
-    float v[8], a[8];
-    load8<DT>(dy + i * lddy + j, n, v);
-    load8<DT>(z + i * ldz + j, n, a);
-    times_slope8(v, a, act);
-    store8<DT>(dz + i * lddz + j, n, v);
+    float v[1][8], a[1][8];
+    load8<DT>(dy + i * lddy + j, n, v[0]);
+    load8<DT>(z + i * ldz + j, n, a[0]);
+    times_slope8<1>(v, a, act);
+    store8<DT>(dz + i * lddz + j, n, v[0]);
 }
 
 template <int DT>

@@ -63,12 +63,21 @@ __device__ __forceinline__ void each(F f) {
     each_of(std::make_integer_sequence<int, N>{}, f);
 }
 
+// A barrier that waits for the wave's accesses to LDS but not for those to memory, as __syncthreads() would
+__device__ __forceinline__ void meet() {
+    asm volatile("" : : : "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);        // lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" : : : "memory");
+}
+
 struct Args {
     const unsigned char* a;
     const unsigned char* b;
     long long lda, ldb;                       // bytes
     unsigned long long a_span, b_span;        // bytes from the first element to behind the last
     int I, J, C, c_per, tiles_i, tiles_j;
+    unsigned work;                            // tiles x splits
     Finish f;
     float* parts;
 };
@@ -81,48 +90,64 @@ struct Beside {
         if (f.add) add.load(static_cast<const T*>(f.add) + i * f.ld_add + j, n);
         if (f.kind == kGradInput && f.zin) zin.load(static_cast<const T*>(f.zin) + i * f.ld_zin + j, n);
     }
+    template <bool ADD, bool ZIN>
+    __device__ __forceinline__ void load_whole(const Finish& f, long long i, int j) {
+        if constexpr (ADD) add.load_whole(static_cast<const T*>(f.add) + i * f.ld_add + j);
+        if constexpr (ZIN) zin.load_whole(static_cast<const T*>(f.zin) + i * f.ld_zin + j);
+    }
 };
 
-// Results v[0..7] at (i, j..j+7), n of them inside the matrix
-__device__ __forceinline__ void finish8(const Finish& f, float v[8], const float bias[8], const Beside& beside, long long i, int j, int n) {
+// Results v[r][0..7] at (i + r * between, j..j+7), n of them inside the matrix.  ADD, ZIN: there may be such an operand
+template <bool ADD, bool ZIN, int R>
+__device__ __forceinline__ void finish_rows(const Finish& f, float v[R][8], const float bias[8], const Beside beside[R], long long i,
+                                            int between, int j, int n) {
     if (f.kind == kFloat) {
-        store8<PCONV_F32>(static_cast<float*>(f.out) + i * f.ld_out + j, n, v);
+#pragma unroll
+        for (int r = 0; r < R; ++r) store8<PCONV_F32>(static_cast<float*>(f.out) + (i + r * between) * f.ld_out + j, n, v[r]);
         return;
     }
-    float add[8] = {};
-    if (f.add) beside.add.get(add);
+    auto plus = [&] {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float add[8];
+            beside[r].add.get(add);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v[r][q] += add[q];
+        }
+    };
     if (f.kind == kForward) {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] += bias[q];
-        if (f.add && f.first)
+        for (int r = 0; r < R; ++r)
 #pragma unroll
-            for (int q = 0; q < 8; ++q) v[q] += add[q];
-        if (f.z) store8<DT>(static_cast<T*>(f.z) + i * f.ld_out + j, n, v);
-        activate8(v, f.act);
-        if (f.add && !f.first)
+            for (int q = 0; q < 8; ++q) v[r][q] += bias[q];
+        if (ADD && f.add && f.first) plus();
+        if (f.z)
 #pragma unroll
-            for (int q = 0; q < 8; ++q) v[q] += add[q];
+            for (int r = 0; r < R; ++r) store8<DT>(static_cast<T*>(f.z) + (i + r * between) * f.ld_out + j, n, v[r]);
+        activate8<R>(v, f.act);
+        if (ADD && f.add && !f.first) plus();
     } else {
-        if (f.zin) {
-            float z[8];
-            beside.zin.get(z);
-            times_slope8(v, z, f.act);
-        }
-        if (f.add)
+        if (ZIN && f.zin) {
 #pragma unroll
-            for (int q = 0; q < 8; ++q) v[q] += add[q];
+            for (int r = 0; r < R; ++r) {
+                float z[1][8];
+                beside[r].zin.get(z[0]);
+                times_slope8<1>(v + r, z, f.act);
+            }
+        }
+        if (ADD && f.add) plus();
     }
-    store8<DT>(static_cast<T*>(f.out) + i * f.ld_out + j, n, v);
+#pragma unroll
+    for (int r = 0; r < R; ++r) store8<DT>(static_cast<T*>(f.out) + (i + r * between) * f.ld_out + j, n, v[r]);
+}
+__device__ __forceinline__ void finish8(const Finish& f, float v[1][8], const float bias[8], long long i, int j, int n) {
+    Beside beside[1];
+    beside[0].load(f, i, j, n);
+    finish_rows<true, true, 1>(f, v, bias, beside, i, 0, j, n);
 }
 __device__ __forceinline__ void bias8(const Finish& f, int j, int n, float bias[8]) {
 #pragma unroll
     for (int q = 0; q < 8; ++q) bias[q] = f.kind == kForward && f.bias && q < n ? f.bias[j + q] : 0.f;
-}
-
-// Workgroup b of G onto the work in order: consecutive workgroups go to different XCDs, an XCD's workgroups take consecutive work.
-__device__ __forceinline__ unsigned by_xcd(unsigned b, unsigned G) {
-    const unsigned x = b % 8, q = G / 8, r = G % 8;
-    return x * q + (x < r ? x : r) + b / 8;
 }
 
 // How one operand of W rows (i or j) is staged and read.  ROWS: stored with c across its rows.
@@ -184,43 +209,60 @@ __global__ __launch_bounds__(WI * WJ * 64) void product_kernel(const Args p) {
     constexpr int THREADS = WI * WJ * 64, TI = 16 * AF * WI, TJ = 16 * BF * WJ;
     typedef Operand<AR, TI, THREADS> OA;
     typedef Operand<BR, TJ, THREADS> OB;
-    constexpr int STAGE = OA::kBytes + OB::kBytes;
+    // LDS: three stages of A, two of B; a wave's window for the results lies in the stage of A that is not in use then
+    constexpr int B_AT = 3 * OA::kBytes;
     extern __shared__ __align__(16) unsigned char lds[];
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int wi = wave % WI, wj = wave / WI;
 
-    // tile: groups of eight tile rows, column by column inside a group
-    const unsigned tiles = (unsigned)p.tiles_i * p.tiles_j;
-    const unsigned id = by_xcd(blockIdx.x, gridDim.x), split = id / tiles, tile = id % tiles;
-    const unsigned per_group = 8u * p.tiles_j, group = tile / per_group, in = tile % per_group;
-    const unsigned high = min(8u, (unsigned)p.tiles_i - group * 8);
-    const int i0 = (int)(group * 8 + in % high) * TI, j0 = (int)(in / high) * TJ;
-    const int c0 = (int)split * p.c_per, c1 = min(p.C, c0 + p.c_per);
-    const int stages = (c1 - c0 + BK - 1) / BK;
-
-    // where the operands' next stage begins, and the bytes from there to the matrix's end
-    const unsigned long long a_at = AR ? (unsigned long long)c0 * p.lda + (unsigned long long)i0 * ES
-                                       : (unsigned long long)i0 * p.lda + (unsigned long long)c0 * ES;
-    const unsigned long long b_at = BR ? (unsigned long long)c0 * p.ldb + (unsigned long long)j0 * ES
-                                       : (unsigned long long)j0 * p.ldb + (unsigned long long)c0 * ES;
-    const unsigned char *pa = p.a + a_at, *pb = p.b + b_at;
-    unsigned long long a_left = p.a_span - a_at, b_left = p.b_span - b_at;
+    // The workgroups of an XCD (every eighth) take turns along a range of the work of their own.  A piece of work: a split of c and a
+    // tile, tiles in groups of eight tile rows, column by column inside a group, so that those under way at a time share operands.
+    const unsigned tiles = (unsigned)p.tiles_i * p.tiles_j, xcd = blockIdx.x % 8, turn = gridDim.x / 8;
+    const unsigned first = (unsigned)((unsigned long long)p.work * xcd / 8) + blockIdx.x / 8;
+    const unsigned end = (unsigned)((unsigned long long)p.work * (xcd + 1) / 8);
+    if (first >= end) return;
+    // Where a piece of work's operands begin, the bytes from there to the matrices' ends, and how much of c is left; none: zeros
+    struct Work {
+        int i0, j0, split, stages;
+        const unsigned char *pa, *pb;
+        unsigned long long a_left, b_left;
+        int c_left;
+    };
     const unsigned long long a_step = AR ? (unsigned long long)p.lda * BK : kStageBytes;
     const unsigned long long b_step = BR ? (unsigned long long)p.ldb * BK : kStageBytes;
-    int c_left = c1 - c0;
-
+    auto work_at = [&](unsigned id) {
+        Work w{};
+        if (id >= end) return w;
+        const unsigned split = id / tiles, tile = id % tiles;
+        const unsigned per_group = 8u * p.tiles_j, group = tile / per_group, in = tile % per_group;
+        const unsigned high = min(8u, (unsigned)p.tiles_i - group * 8);
+        const int c0 = (int)split * p.c_per;
+        w.i0 = (int)(group * 8 + in % high) * TI;
+        w.j0 = (int)(in / high) * TJ;
+        w.split = (int)split;
+        w.c_left = min(p.C, c0 + p.c_per) - c0;
+        w.stages = max(2, (w.c_left + BK - 1) / BK);           // (two at least, the second of zeros where there is one: see main_loop)
+        const unsigned long long a_at = AR ? (unsigned long long)c0 * p.lda + (unsigned long long)w.i0 * ES
+                                           : (unsigned long long)w.i0 * p.lda + (unsigned long long)c0 * ES;
+        const unsigned long long b_at = BR ? (unsigned long long)c0 * p.ldb + (unsigned long long)w.j0 * ES
+                                           : (unsigned long long)w.j0 * p.ldb + (unsigned long long)c0 * ES;
+        w.pa = p.a + a_at;
+        w.pb = p.b + b_at;
+        w.a_left = p.a_span - a_at;
+        w.b_left = p.b_span - b_at;
+        return w;
+    };
+    Work now = work_at(first);
+    // the operands' next stage
+    const unsigned char *pa = now.pa, *pb = now.pb;
+    unsigned long long a_left = now.a_left, b_left = now.b_left;
+    int c_left = now.c_left;
     float4v acc[AF][BF];
-#pragma unroll
-    for (int a = 0; a < AF; ++a)
-#pragma unroll
-        for (int b = 0; b < BF; ++b) acc[a][b] = float4v{0.f, 0.f, 0.f, 0.f};
 
     // DIRECT: the stage that is being asked for, a piece at a time
-    constexpr int PIECES = OA::kPieces + OB::kPieces;
     __amdgpu_buffer_rsrc_t rsrc_a, rsrc_b;
     unsigned off_a[OA::kVariants], off_b[OB::kVariants];
-    int to_stage = 0;
-    auto begin_stage = [&](int buf) {
+    auto begin_stage = [&] {
         auto offsets = [&](auto tag, long long ld, unsigned* off) {
             typedef decltype(tag) O;
 #pragma unroll
@@ -230,28 +272,27 @@ __global__ __launch_bounds__(WI * WJ * 64) void product_kernel(const Args p) {
                 off[v] = !O::kRows && piece * PER >= c_left ? kInvalid : (unsigned)(line * ld) + piece * 16;
             }
         };
-        // (behind the last stage nothing is there: zeros, which nobody reads)
+        // (where nothing is left: zeros)
         rsrc_a = make_rsrc(pa, c_left > 0 ? (uint32_t)min(a_left, 0x7FFFFFFFull) : 0);
         rsrc_b = make_rsrc(pb, c_left > 0 ? (uint32_t)min(b_left, 0x7FFFFFFFull) : 0);
         offsets(OA{}, p.lda, off_a);
         offsets(OB{}, p.ldb, off_b);
-        to_stage = buf * STAGE + wave * 1024;
         pa += a_step;
         pb += b_step;
         a_left -= a_step;
         b_left -= b_step;
         c_left -= BK;
     };
-    auto ask_piece = [&](lds_bytes into, int q) {
-        if (q < OA::kPieces) {
-            const int v = q % OA::kVariants;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_a, (lds_ptr)(into + to_stage + q * THREADS * 16), 16,
-                                                     (int)(off_a[v] + (unsigned)((q - v) * OA::kLinesPer * p.lda)), 0, 0, 0);
-        } else {
-            const int o = q - OA::kPieces, v = o % OB::kVariants;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_b, (lds_ptr)(into + to_stage + OA::kBytes + o * THREADS * 16), 16,
-                                                     (int)(off_b[v] + (unsigned)((o - v) * OB::kLinesPer * p.ldb)), 0, 0, 0);
-        }
+    // piece q of an operand's stage, into the LDS at `to`
+    auto ask_a = [&](lds_bytes to, int q) {
+        const int v = q % OA::kVariants;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_a, (lds_ptr)(to + wave * 1024 + q * THREADS * 16), 16,
+                                                 (int)(off_a[v] + (unsigned)((q - v) * OA::kLinesPer * p.lda)), 0, 0, 0);
+    };
+    auto ask_b = [&](lds_bytes to, int q) {
+        const int v = q % OB::kVariants;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_b, (lds_ptr)(to + wave * 1024 + q * THREADS * 16), 16,
+                                                 (int)(off_b[v] + (unsigned)((q - v) * OB::kLinesPer * p.ldb)), 0, 0, 0);
     };
     // through registers: a stage's pieces
     uint4v ra[DIRECT ? 1 : OA::kPieces], rb[DIRECT ? 1 : OB::kPieces];
@@ -267,34 +308,145 @@ __global__ __launch_bounds__(WI * WJ * 64) void product_kernel(const Args p) {
         }
     };
     auto fetch_stage = [&] {
-        fetch(OA{}, pa, p.lda, p.I - i0, ra);
-        fetch(OB{}, pb, p.ldb, p.J - j0, rb);
+        fetch(OA{}, pa, p.lda, p.I - now.i0, ra);
+        fetch(OB{}, pb, p.ldb, p.J - now.j0, rb);
         pa += a_step;
         pb += b_step;
         c_left -= BK;
     };
     auto put_stage = [&](int buf) {
         if constexpr (!DIRECT) {
-            unsigned char* const to = lds + buf * STAGE;
 #pragma unroll
-            for (int q = 0; q < OA::kPieces; ++q) *reinterpret_cast<uint4v*>(to + (q * THREADS + t) * 16) = ra[q];
+            for (int q = 0; q < OA::kPieces; ++q) *reinterpret_cast<uint4v*>(lds + buf * OA::kBytes + (q * THREADS + t) * 16) = ra[q];
 #pragma unroll
-            for (int q = 0; q < OB::kPieces; ++q) *reinterpret_cast<uint4v*>(to + OA::kBytes + (q * THREADS + t) * 16) = rb[q];
+            for (int q = 0; q < OB::kPieces; ++q) *reinterpret_cast<uint4v*>(lds + B_AT + buf * OB::kBytes + (q * THREADS + t) * 16) = rb[q];
         }
     };
 
     typedef uint4v FragA[AF];
     typedef uint4v FragB[BF];
-    auto read_one = [&](lds_bytes from, int buf, int k, int q, FragA& fa, FragB& fb) {
-        const lds_bytes la = from + buf * STAGE, lb = la + OA::kBytes;
+    auto read_one = [&](lds_bytes la, lds_bytes lb, int k, int q, FragA& fa, FragB& fb) {
         if (q < BF) fb[q] = OB::read(lb, wj * BF + q, k, lane);
         else fa[q - BF] = OA::read(la, wi * AF + q - BF, k, lane);
     };
+    auto clear = [&] {
+#pragma unroll
+        for (int a = 0; a < AF; ++a)
+#pragma unroll
+            for (int b = 0; b < BF; ++b) acc[a][b] = float4v{0.f, 0.f, 0.f, 0.f};
+    };
+    // Results leave through a window of 16 i x 16 BF j floats for each wave; of a row's 16-byte pieces, piece q lies at q ^ row, which
+    // spreads the rows over the banks.
+    constexpr int PITCH = 16 * BF * 4, ROW_LANES = 2 * BF, ROWS_AT_ONCE = 64 / ROW_LANES, TIMES = 16 / ROWS_AT_ONCE;
+    static_assert(16 % ROWS_AT_ONCE == 0 && WI * WJ * 16 * PITCH <= OA::kBytes, "the windows fit a stage of A");
+    constexpr int SPREAD = 4 * BF < 16 ? 4 * BF - 1 : 15;
+    auto put_block = [&](unsigned char* win, const float4v (&block)[BF]) {
+        const int row = lane & 15;
+#pragma unroll
+        for (int b = 0; b < BF; ++b) {
+            float4v v;
+            asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v.x) : "a"(block[b].x));
+            asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v.y) : "a"(block[b].y));
+            asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v.z) : "a"(block[b].z));
+            asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v.w) : "a"(block[b].w));
+            *reinterpret_cast<float4v*>(win + row * PITCH + ((b * 4 + (lane >> 4)) ^ (row & SPREAD)) * 16) = v;
+        }
+    };
+    auto finish = [&](int at) {
+        unsigned char* const win = lds + at + wave * 16 * PITCH;
+        // (the reads of accumulators in put_block are the assembler's: no wait is put in front of them; the last MFMA, of 8 passes at
+        // most, is done 11 wait states behind it)
+        asm volatile("s_nop 15\n\ts_nop 15");
+        Finish f = p.f;
+        if (p.parts) {
+            f.kind = kFloat;
+            f.out = p.parts + (unsigned long long)now.split * p.I * p.J;
+            f.ld_out = p.J;
+        }
+        const int j = now.j0 + wj * 16 * BF + (lane % ROW_LANES) * 8, n = p.J - j, i_first = now.i0 + wi * AF * 16 + lane / ROW_LANES;
+        float bias[8];
+        bias8(f, j, n, bias);
+        auto put = [&](int a) {
+#pragma unroll
+            for (int b = 0; b < AF; ++b)
+                if (a == b) put_block(win, acc[b]);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        };
+        auto get = [&](int r, float (&v)[8]) {
+            const int row = lane / ROW_LANES + r * ROWS_AT_ONCE, q = (lane % ROW_LANES) * 2;
+            const float4v lo = *reinterpret_cast<const float4v*>(win + row * PITCH + (q ^ (row & SPREAD)) * 16);
+            const float4v hi = *reinterpret_cast<const float4v*>(win + row * PITCH + ((q + 1) ^ (row & SPREAD)) * 16);
+            v[0] = lo.x; v[1] = lo.y; v[2] = lo.z; v[3] = lo.w;
+            v[4] = hi.x; v[5] = hi.y; v[6] = hi.z; v[7] = hi.w;
+        };
+        auto done = [&] {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        };
+        if (now.i0 + TI <= p.I && now.j0 + TJ <= p.J) {
+            // A whole tile, with what it reads besides known to the compiler: loads in a branch, or none, would be waited for in front of
+            // every window, and with them the stores of the window before.
+            auto whole = [&](auto kind, auto add, auto zin) {
+                f.kind = kind;
+                if constexpr (!add) f.add = nullptr;
+                if constexpr (!zin) f.zin = nullptr;
+                Beside next[TIMES];
+                auto load = [&](int a) {
+                    if constexpr (add || zin)
+#pragma unroll
+                        for (int r = 0; r < TIMES; ++r) next[r].template load_whole<add, zin>(f, i_first + a * 16 + r * ROWS_AT_ONCE, j);
+                };
+                load(0);
+#pragma unroll 1
+                for (int a = 0; a < AF; ++a) {
+                    Beside beside[TIMES];
+#pragma unroll
+                    for (int r = 0; r < TIMES; ++r) beside[r] = next[r];
+                    put(a);
+                    load(a + 1 < AF ? a + 1 : a);
+                    float v[TIMES][8];
+#pragma unroll
+                    for (int r = 0; r < TIMES; ++r) get(r, v[r]);
+                    finish_rows<add, zin, TIMES>(f, v, bias, beside, i_first + a * 16, ROWS_AT_ONCE, j, 8);
+                    done();
+                }
+            };
+            constexpr std::true_type yes{};
+            constexpr std::false_type no{};
+            if (f.kind == kFloat) whole(std::integral_constant<int, kFloat>{}, no, no);
+            else if constexpr (!BR) {
+                if (f.add) whole(std::integral_constant<int, kForward>{}, yes, no);
+                else whole(std::integral_constant<int, kForward>{}, no, no);
+            } else if constexpr (!AR) {
+                if (f.add && f.zin) whole(std::integral_constant<int, kGradInput>{}, yes, yes);
+                else if (f.add) whole(std::integral_constant<int, kGradInput>{}, yes, no);
+                else if (f.zin) whole(std::integral_constant<int, kGradInput>{}, no, yes);
+                else whole(std::integral_constant<int, kGradInput>{}, no, no);
+            }
+            return;
+        }
+#pragma unroll 1
+        for (int a = 0; a < AF; ++a) {
+            put(a);
+#pragma unroll 1
+            for (int r = 0; r < TIMES; ++r) {
+                const int i = i_first + a * 16 + r * ROWS_AT_ONCE;
+                float v[1][8];
+                get(r, v[0]);
+                if (i < p.I && n > 0) finish8(f, v, bias, i, j, n);
+            }
+            done();
+        }
+    };
+
     if constexpr (DIRECT) {
-        // A step's operands are read while the step before is multiplied, across stages too: the barrier that publishes stage
-        // s + 1 stands in front of stage s's last step, whose operands are in registers by then, so that stage s + 2 can be asked
-        // for into the same half: a piece at a time between the MFMAs of that step (asked for together they stand in the way of
-        // every wave's next instructions until the memory pipeline has taken them).
+        // One sequence of stages over all of the workgroup's work.  A step's operands are read while the step before is multiplied,
+        // across stages too: the barrier that publishes stage s + 1 stands in front of stage s's last step, whose operands are in
+        // registers by then.  Stage s + 2 is asked for in the course of stage s, a piece at a time between MFMAs (together they stand in
+        // the way of every wave's next instructions until the memory pipeline has taken them, and workgroups that run in step ask
+        // for more than L2 gives at a time): A in the first step, into a third stage of its own, B in the last one, into stage s's, which
+        // all waves have read then.  At the end of a piece of work the next one's first two stages are in LDS.
         static_assert(KS == 2, "");
         constexpr int MFMAS = AF * BF, READS = AF + BF;
         // (two pointers to the stages, said not to alias, or the compiler waits for every piece that is under way in front of each
@@ -302,103 +454,106 @@ __global__ __launch_bounds__(WI * WJ * 64) void product_kernel(const Args p) {
         auto main_loop = [&](const lds_bytes __restrict into, const lds_bytes __restrict from) {
             FragA fa[2];
             FragB fb[2];
-            auto step = [&](auto kk, int buf) {
-                constexpr int k = kk;
+            // where the stages of A lie, s, s + 1, s + 2, and of B, s, s + 1
+            int a0 = 0, a1 = OA::kBytes, a2 = 2 * OA::kBytes, b0 = B_AT, b1 = B_AT + OB::kBytes;
+            auto step = [&](auto kk) {
+                constexpr int k = kk, ASKS = k ? OB::kPieces : OA::kPieces;
                 each<MFMAS>([&](auto mm) {
                     constexpr int m = mm;
                     // (behind the last stage: what is there, and not used)
                     each<READS>([&](auto q) {
-                        if constexpr (q * MFMAS / READS == m) read_one(from, k == 0 ? buf : buf ^ 1, k ^ 1, q, fa[k ^ 1], fb[k ^ 1]);
+                        if constexpr (q * MFMAS / READS == m) read_one(from + (k ? a1 : a0), from + (k ? b1 : b0), k ^ 1, q, fa[k ^ 1], fb[k ^ 1]);
                     });
-                    if constexpr (k == 1)
-                        each<PIECES>([&](auto q) {
-                            if constexpr (q * MFMAS / PIECES == m) ask_piece(into, q);
-                        });
+                    each<ASKS>([&](auto q) {
+                        if constexpr ((2 * q + 1) * MFMAS / (2 * ASKS) == m) {
+                            if constexpr (k == 0) ask_a(into + a2, q);
+                            else ask_b(into + b0, q);
+                        }
+                    });
                     acc[m / BF][m % BF] = mma(fb[k][m % BF], fa[k][m / BF], acc[m / BF][m % BF]);
+                    asm volatile("" : "+a"(acc[m / BF][m % BF]));          // (it stays where it is)
                     __builtin_amdgcn_sched_barrier(0);
                 });
             };
             each<2>([&](auto s) {
-                begin_stage(s);
-                each<PIECES>([&](auto q) { ask_piece(into, q); });
+                begin_stage();
+                each<OA::kPieces>([&](auto q) { ask_a(into + s * OA::kBytes, q); });
+                each<OB::kPieces>([&](auto q) { ask_b(into + B_AT + s * OB::kBytes, q); });
             });
-            __builtin_amdgcn_s_waitcnt(0x0F70 | (PIECES & 15) | (PIECES >> 4) << 14);      // vmcnt: all but the pieces of stage 1
+            __builtin_amdgcn_s_waitcnt(0x0F70);                // vmcnt(0)
             __syncthreads();
-            each<READS>([&](auto q) { read_one(from, 0, 0, q, fa[0], fb[0]); });
-            for (int s = 0; s < stages; ++s) {
-                step(std::integral_constant<int, 0>{}, s & 1);
-                __builtin_amdgcn_s_waitcnt(0x0F70);        // vmcnt(0): this wave's pieces of stage s + 1 are in LDS
-                __syncthreads();                           // so are the other waves', and all have read stage s
-                begin_stage(s & 1);
-                __builtin_amdgcn_sched_barrier(0);
-                step(std::integral_constant<int, 1>{}, s & 1);
+            for (unsigned id = first; id < end; id += turn) {
+                const Work then = work_at(id + turn);
+                clear();
+                // (not kept from the last stage before: the registers are needed in between)
+                each<READS>([&](auto q) { read_one(from + a0, from + b0, 0, q, fa[0], fb[0]); });
+                // (no branch in this loop: with one the accumulators are copied from block to block)
+                for (int s = 0, more = 1; more; ++s) {
+                    const bool over = s == now.stages - 2;     // the work's last stage has been asked for: the next one's first two
+                    pa = over ? then.pa : pa;
+                    pb = over ? then.pb : pb;
+                    a_left = over ? then.a_left : a_left;
+                    b_left = over ? then.b_left : b_left;
+                    c_left = over ? then.c_left : c_left;
+                    begin_stage();
+                    __builtin_amdgcn_sched_barrier(0);
+                    step(std::integral_constant<int, 0>{});
+                    // this wave's pieces of stage s + 1 are in LDS: all but those of A that were asked for just now; stage 1's have been
+                    // waited for
+                    asm volatile("s_cmp_eq_u32 %0, 0\n\ts_cbranch_scc1 .Lthere%=\n\ts_waitcnt vmcnt(%1)\n.Lthere%=:" : : "s"(s), "i"(OA::kPieces) : "scc", "memory");
+                    meet();                                    // so are the other waves', and all have read stage s
+                    __builtin_amdgcn_sched_barrier(0);
+                    step(std::integral_constant<int, 1>{});
+                    const int a = a0, b = b0;
+                    a0 = a1;
+                    a1 = a2;
+                    a2 = a;
+                    b0 = b1;
+                    b1 = b;
+                    more = now.stages - 1 - s;
+                    asm("" : "+s"(more));                      // (or it peels the last stage off)
+                }
+                // (vmcnt(0), here: the wait in stage 0 would be one for the results' stores too)
+                __builtin_amdgcn_s_waitcnt(0x0F70);
+                finish(a2);
+                meet();                                        // the windows are free again
+                now = then;
             }
         };
         lds_bytes into = (lds_bytes)lds, from = into;
         asm("" : "+s"(into), "+s"(from));              // (or it knows that they are the same)
         main_loop(into, from);
-        __builtin_amdgcn_s_waitcnt(0x0F70);
     } else {
-        fetch_stage();
-        put_stage(0);
-        for (int s = 0; s < stages; ++s) {
-            const int buf = s & 1;
-            __syncthreads();                   // stage s is in LDS for every wave, and no wave reads the other half any more
-            if (s + 1 < stages) fetch_stage();
+        for (unsigned id = first; id < end; id += turn) {
+            now = work_at(id);
+            pa = now.pa;
+            pb = now.pb;
+            c_left = now.c_left;
+            clear();
+            fetch_stage();
+            put_stage(0);
+            for (int s = 0; s < now.stages; ++s) {
+                const int buf = s & 1;
+                __syncthreads();                   // stage s is in LDS for every wave, and no wave reads the other half any more
+                if (s + 1 < now.stages) fetch_stage();
 #pragma unroll
-            for (int k = 0; k < KS; ++k) {
-                FragA fa;
-                FragB fb;
+                for (int k = 0; k < KS; ++k) {
+                    FragA fa;
+                    FragB fb;
 #pragma unroll
-                for (int q = 0; q < AF + BF; ++q) read_one((lds_bytes)lds, buf, k, q, fa, fb);
+                    for (int q = 0; q < AF + BF; ++q)
+                        read_one((lds_bytes)(lds + buf * OA::kBytes), (lds_bytes)(lds + B_AT + buf * OB::kBytes), k, q, fa, fb);
 #pragma unroll
-                for (int m = 0; m < AF * BF; ++m) acc[m / BF][m % BF] = mma(fb[m % BF], fa[m / BF], acc[m / BF][m % BF]);
+                    for (int m = 0; m < AF * BF; ++m) {
+                        acc[m / BF][m % BF] = mma(fb[m % BF], fa[m / BF], acc[m / BF][m % BF]);
+                        asm volatile("" : "+a"(acc[m / BF][m % BF]));
+                    }
+                }
+                if (s + 1 < now.stages) put_stage(buf ^ 1);
             }
-            if (s + 1 < stages) put_stage(buf ^ 1);
+            finish(2 * OA::kBytes);
+            __syncthreads();
         }
-    }
-    __syncthreads();
-
-    // results: a window of 16 i x 16 BF j floats for each wave, a pitch that spreads the rows over the banks
-    constexpr int PITCH = (16 * BF + 4) * 4, ROW_LANES = 2 * BF, ROWS_AT_ONCE = 64 / ROW_LANES;
-    static_assert(WI * WJ * 16 * PITCH <= 2 * STAGE && 16 % ROWS_AT_ONCE == 0, "the windows fit the stages");
-    unsigned char* const win = lds + wave * 16 * PITCH;
-    Finish f = p.f;
-    if (p.parts) {
-        f.kind = kFloat;
-        f.out = p.parts + (unsigned long long)split * p.I * p.J;
-        f.ld_out = p.J;
-    }
-    const int j = j0 + wj * 16 * BF + (lane % ROW_LANES) * 8, n = p.J - j;
-    float bias[8];
-    bias8(f, j, n, bias);
-    auto put_block = [&](const float4v (&block)[BF]) {
-#pragma unroll
-        for (int b = 0; b < BF; ++b)
-            *reinterpret_cast<float4v*>(win + (lane & 15) * PITCH + (b * 16 + (lane >> 4) * 4) * 4) = block[b];
-    };
-    constexpr int TIMES = 16 / ROWS_AT_ONCE;
-#pragma unroll 1
-    for (int a = 0; a < AF; ++a) {
-        const int i = i0 + (wi * AF + a) * 16 + lane / ROW_LANES;
-        Beside beside[TIMES];
-#pragma unroll
-        for (int r = 0; r < TIMES; ++r)
-            if (i + r * ROWS_AT_ONCE < p.I) beside[r].load(f, i + r * ROWS_AT_ONCE, j, n);
-#pragma unroll
-        for (int b = 0; b < AF; ++b)
-            if (a == b) put_block(acc[b]);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int r = 0; r < TIMES; ++r) {
-            const unsigned char* const at = win + (lane / ROW_LANES + r * ROWS_AT_ONCE) * PITCH + (lane % ROW_LANES) * 32;
-            const float4v lo = *reinterpret_cast<const float4v*>(at), hi = *reinterpret_cast<const float4v*>(at + 16);
-            float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-            if (i + r * ROWS_AT_ONCE < p.I && n > 0) finish8(f, v, bias, beside[r], i + r * ROWS_AT_ONCE, j, n);
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -409,16 +564,14 @@ __global__ __launch_bounds__(256) void add_parts_kernel(const float* parts, int 
     const unsigned long long i = at / per_row;
     if (i >= (unsigned long long)I) return;
     const int j = (int)(at % per_row) * 8, n = J - j;
-    float v[8] = {}, w[8], bias[8];
+    float v[1][8] = {}, w[8], bias[8];
     for (int s = 0; s < splits; ++s) {
         load8<PCONV_F32>(parts + ((unsigned long long)s * I + i) * J + j, n, w);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] += w[q];
+        for (int q = 0; q < 8; ++q) v[0][q] += w[q];
     }
     bias8(f, j, n, bias);
-    Beside beside;
-    beside.load(f, (long long)i, j, n);
-    finish8(f, v, bias, beside, (long long)i, j, n);
+    finish8(f, v, bias, (long long)i, j, n);
 }
 
 // Few rows of x (up to 16) with weights that are read once, straight into registers: memory bounds it, no operand is shared.  A
@@ -464,10 +617,10 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_rows_kernel(const Args p) 
     if (t < 32) {
         const int i = t >> 1, j = j0 + (t & 1) * 8, n = p.J - j;
         if (i < p.I && n > 0) {
-            float v[8] = {}, bias[8];
+            float v[1][8] = {}, bias[8];
             for (int s = 0; s < kFewWaves; ++s)
 #pragma unroll
-                for (int q = 0; q < 8; ++q) v[q] += sums[s][i][(t & 1) * 8 + q];
+                for (int q = 0; q < 8; ++q) v[0][q] += sums[s][i][(t & 1) * 8 + q];
             Finish f = p.f;
             if (p.parts) {
                 f.kind = kFloat;
@@ -475,9 +628,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_rows_kernel(const Args p) 
                 f.ld_out = p.J;
             }
             bias8(f, j, n, bias);
-            Beside beside;
-            beside.load(f, i, j, n);
-            finish8(f, v, bias, beside, i, j, n);
+            finish8(f, v, bias, i, j, n);
         }
     }
 }
@@ -514,16 +665,19 @@ int add_parts(const Product& p, hipStream_t st) {
 template <bool AR, bool BR, int WI, int WJ, int AF, int BF>
 int launch_tile(const Product& p, bool direct, hipStream_t st) {
     constexpr int TI = 16 * AF * WI, TJ = 16 * BF * WJ;
-    const Args a = make_args(p, TI, TJ);
-    const size_t lds = 2 * (size_t)(TI + TJ) * kStageBytes;
-    const unsigned long long grid = (unsigned long long)a.tiles_i * a.tiles_j * p.splits;
-    if (grid > 0x7FFFFFFFull) return PCONV_EUNSUPPORTED;
+    Args a = make_args(p, TI, TJ);
+    constexpr size_t lds = (3 * TI + 2 * TJ) * (size_t)kStageBytes;
+    const unsigned long long work = (unsigned long long)a.tiles_i * a.tiles_j * p.splits;
+    if (work > 0x7FFFFFFFull) return PCONV_EUNSUPPORTED;
+    a.work = (unsigned)work;
+    // as many workgroups as are resident, the same number on each XCD
+    const unsigned grid = (unsigned)std::min<unsigned long long>((work + 7) / 8 * 8, kComputeUnits * (160 * 1024 / lds));
 #define PCONV_PRODUCT(DIRECT)                                                                                           \
     {                                                                                                                   \
         auto kern = product_kernel<AR, BR, WI, WJ, AF, BF, DIRECT>;                                                     \
         static LdsAllowance allowed;                                                                                    \
         if (lds > 64 * 1024) PCONV_HIP(allowed.ask((const void*)kern));                                                 \
-        hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(WI * WJ * 64), lds, st, a);                                 \
+        hipLaunchKernelGGL(kern, dim3(grid), dim3(WI * WJ * 64), lds, st, a);                                 \
     }
     if (direct) PCONV_PRODUCT(true) else PCONV_PRODUCT(false)
 #undef PCONV_PRODUCT
