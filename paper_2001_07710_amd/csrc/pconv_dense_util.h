@@ -120,29 +120,35 @@ __device__ __forceinline__ void store8(typename Store<DT>::T* p, int n, const fl
 
 constexpr float kSqrtHalf = 0.70710678118654752f, kSqrt2OverPi = 0.79788456080286536f, kInvSqrt2Pi = 0.39894228040143268f;
 
-// z moved into +-100, NaN left as it is: behind that an activation's curve is 0 or 1 (times z) in 32 bits, and no inf * 0 arises
+// z moved into +-100: behind that an activation's curve is 0 or 1 (times z) in 32 bits, and no inf * 0 arises.  `tamed` leaves NaN as it
+// is; `bounded`, one instruction, does not: for curves, which z itself multiplies.
 __device__ __forceinline__ float tamed(float z) { return z > 100.f ? 100.f : z < -100.f ? -100.f : z; }
+__device__ __forceinline__ float bounded(float z) { return __builtin_amdgcn_fmed3f(z, -100.f, 100.f); }
+// 1 / (1 + 2^x).  (v_exp_f32 and v_rcp_f32 are good to one unit of 32 bits each; an IEEE division is ten instructions.)
+__device__ __forceinline__ float falling(float x) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x)); }
+constexpr float kLog2E = 1.44269504088896341f;
 
 __device__ __forceinline__ float relu(float z) { return z < 0.f ? 0.f : z; }                    // (NaN stays)
 __device__ __forceinline__ float relu_slope(float z) { return z > 0.f ? 1.f : z == z ? 0.f : z; }
-__device__ __forceinline__ float gelu(float z) { return z * (0.5f + 0.5f * erff(tamed(z) * kSqrtHalf)); }
+__device__ __forceinline__ float gelu(float z) { return z * (0.5f + 0.5f * erff(bounded(z) * kSqrtHalf)); }
 __device__ __forceinline__ float gelu_slope(float z) {
     const float t = tamed(z);
-    return 0.5f + 0.5f * erff(t * kSqrtHalf) + t * kInvSqrt2Pi * __expf(-0.5f * t * t);
+    return 0.5f + 0.5f * erff(t * kSqrtHalf) + t * kInvSqrt2Pi * __builtin_amdgcn_exp2f(-0.5f * kLog2E * t * t);
 }
 // (1 + tanh(u)) / 2 = 1 / (1 + exp(-2u)): no cancellation where the curve nears 0
 __device__ __forceinline__ float gelu_tanh_share(float t) {
-    return 1.f / (1.f + __expf(-2.f * kSqrt2OverPi * (t + 0.044715f * t * t * t)));
+    constexpr float k = -2.f * kSqrt2OverPi * kLog2E;
+    return falling(t * fmaf(k * 0.044715f, t * t, k));
 }
-__device__ __forceinline__ float gelu_tanh(float z) { return z * gelu_tanh_share(tamed(z)); }
+__device__ __forceinline__ float gelu_tanh(float z) { return z * gelu_tanh_share(bounded(z)); }
 __device__ __forceinline__ float gelu_tanh_slope(float z) {
     const float t = tamed(z), s = gelu_tanh_share(t);
-    return s + t * s * (1.f - s) * (2.f * kSqrt2OverPi) * (1.f + 3.f * 0.044715f * t * t);
+    return fmaf(t * s * (1.f - s), fmaf(6.f * kSqrt2OverPi * 0.044715f, t * t, 2.f * kSqrt2OverPi), s);
 }
-__device__ __forceinline__ float silu(float z) { return z * (1.f / (1.f + __expf(-tamed(z)))); }
+__device__ __forceinline__ float silu(float z) { return z * falling(-kLog2E * bounded(z)); }
 __device__ __forceinline__ float silu_slope(float z) {
-    const float t = tamed(z), s = 1.f / (1.f + __expf(-t));
-    return s * (1.f + t * (1.f - s));
+    const float t = tamed(z), s = falling(-kLog2E * t);
+    return s * fmaf(t, 1.f - s, 1.f);
 }
 
 // v = curve(v), or v *= slope(z), for R times eight values

@@ -97,12 +97,28 @@ __global__ __launch_bounds__(256) void column_sums_kernel(const typename Store<D
         store8<PCONV_F32>(out + (size_t)blockIdx.y * N + j, n, sum);
     }
 }
+// 64 columns a workgroup, 16 threads to four of them, each with every 16th strip
 __global__ __launch_bounds__(256) void add_strips_kernel(const float* parts, int strips, int N, float* out) {
-    const int j = blockIdx.x * 256 + threadIdx.x;
-    if (j >= N) return;
-    float sum = 0.f;
-    for (int s = 0; s < strips; ++s) sum += parts[(size_t)s * N + j];
-    out[j] = sum;
+    __shared__ float sums[16][64];
+    const int c = threadIdx.x % 16 * 4, s = threadIdx.x / 16, j = blockIdx.x * 64 + c, n = N - j;
+    float sum[4] = {};
+    if (n > 0)
+#pragma unroll 4
+        for (int g = s; g < strips; g += 16) {
+            const float4v v = __builtin_bit_cast(float4v, load_part<PCONV_F32>(parts + (size_t)g * N + j, n));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] += v[e];
+        }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sums[s][c + e] = sum[e];
+    __syncthreads();
+    const int d = blockIdx.x * 64 + threadIdx.x;
+    if (threadIdx.x < 64 && d < N) {
+        float all = 0.f;
+#pragma unroll
+        for (int q = 0; q < 16; ++q) all += sums[q][threadIdx.x];
+        out[d] = all;
+    }
 }
 __global__ __launch_bounds__(256) void fill_zero_kernel(float* out, unsigned long long n) {
     const unsigned long long i = (unsigned long long)blockIdx.x * 256 + threadIdx.x;
@@ -116,7 +132,7 @@ int column_sums(const void* m, long long ld, int M, int N, float* parts, float* 
                        static_cast<const typename Store<DT>::T*>(m), ld, M, N, per, strips > 1 ? parts : out);
     PCONV_HIP(hipGetLastError());
     if (strips > 1) {
-        hipLaunchKernelGGL(add_strips_kernel, dim3((N + 255) / 256), dim3(256), 0, st, parts, strips, N, out);
+        hipLaunchKernelGGL(add_strips_kernel, dim3((N + 63) / 64), dim3(256), 0, st, parts, strips, N, out);
         PCONV_HIP(hipGetLastError());
     }
     return PCONV_OK;

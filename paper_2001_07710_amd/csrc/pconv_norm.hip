@@ -46,6 +46,26 @@ struct RowSum {
     }
 };
 
+// A thread's columns of gamma or beta, in wide pieces; `none` where there is no such vector, `outside` behind its end.
+template <int P>
+__device__ __forceinline__ void load_columns(const float* v, int d, int D, float none, float outside, float (&out)[P]) {
+#pragma unroll
+    for (int e = 0; e < P; ++e) out[e] = d + e < D ? none : outside;
+    if (!v) return;
+    if (d + P <= D) {
+#pragma unroll
+        for (int h = 0; h < P; h += 4) {
+            const float4v w = __builtin_bit_cast(float4v, load16(v + d + h));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) out[h + e] = w[e];
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < P; ++e)
+            if (d + e < D) out[e] = v[d + e];
+    }
+}
+
 struct NormArgs {
     const void* x;
     const void* dy;
@@ -91,13 +111,10 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const NormArgs p) {
     rows.load(p.x, p.ldx, first, step, p.rows, p.D, t);
     float gamma[Q][P], beta[Q][P];
 #pragma unroll
-    for (int q = 0; q < Q; ++q)
-#pragma unroll
-        for (int e = 0; e < P; ++e) {
-            const int d = (t + q * TPR) * P + e;
-            gamma[q][e] = d < p.D && p.gamma ? p.gamma[d] : 1.f;
-            beta[q][e] = d < p.D && p.beta ? p.beta[d] : 0.f;
-        }
+    for (int q = 0; q < Q; ++q) {
+        load_columns(p.gamma, (t + q * TPR) * P, p.D, 1.f, 1.f, gamma[q]);
+        load_columns(p.beta, (t + q * TPR) * P, p.D, 0.f, 0.f, beta[q]);
+    }
     const float inv = 1.f / (float)p.D;
     for (long long k = 0; k < turns; ++k) {
         const long long r0 = k * step * U + first;
@@ -186,13 +203,11 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(const NormArgs p) {
     load(first);
     float gamma[Q][P], dg[Q][P], db[Q][P];
 #pragma unroll
-    for (int q = 0; q < Q; ++q)
+    for (int q = 0; q < Q; ++q) {
+        load_columns(p.gamma, (t + q * TPR) * P, p.D, 1.f, 0.f, gamma[q]);
 #pragma unroll
-        for (int e = 0; e < P; ++e) {
-            const int d = (t + q * TPR) * P + e;
-            gamma[q][e] = d < p.D ? p.gamma ? p.gamma[d] : 1.f : 0.f;
-            dg[q][e] = db[q][e] = 0.f;
-        }
+        for (int e = 0; e < P; ++e) dg[q][e] = db[q][e] = 0.f;
+    }
     const float inv = 1.f / (float)p.D;
     for (long long k = 0; k < turns; ++k) {
         const long long r0 = k * step * U + first;
@@ -470,11 +485,13 @@ Spread grad_spread(int pieces) {
 }
 #define PCONV_GRAD_SPREADS(X) X(8, 1, 2) X(16, 1, 2) X(32, 1, 2) X(64, 1, 2) X(64, 2, 1) X(256, 1, 1) X(256, 2, 1) X(512, 2, 1) X(1024, 2, 1)
 
+// 1024 threads for a compute unit: more workgroups read gamma and beta more often than they hide (16384 x 4096, bf16, of 256 threads:
+// one for a compute unit 87 us, two 57, four 45, eight 46)
 constexpr int forward_threads(int tpr) { return tpr > 256 ? tpr : 256; }
 int workgroups(const Spread& s, int rows) {
     const int threads = s.tpr ? forward_threads(s.tpr) : kLong, groups = s.tpr ? threads / s.tpr : 1;
     const long long wanted = ((long long)rows + groups - 1) / groups;
-    return (int)std::min<long long>(wanted, 256ll * (2048 / threads));
+    return (int)std::min<long long>(wanted, 256ll * (1024 / threads));
 }
 // (backward: one workgroup for a compute unit, so that there are few parts to add)
 constexpr int backward_threads(int tpr) { return tpr > 512 ? tpr : 512; }
