@@ -34,9 +34,8 @@ struct Product {
 };
 
 constexpr int kComputeUnits = 256;          // of an MI355X: plans and workspaces are the same whatever device is current
-struct TileShape { int i, j, threads; };
 constexpr int kTiles = 3;
-constexpr TileShape kTileShapes[kTiles] = {{256, 256, 256}, {128, 128, 256}, {64, 64, 256}};
+constexpr int kTileEdges[kTiles] = {256, 128, 64};
 constexpr int kStageBytes = 128;            // of c per stage, of one row
 
 int launch_product_f32(const Product& p, void* stream);

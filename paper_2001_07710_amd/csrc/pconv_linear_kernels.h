@@ -205,7 +205,7 @@ struct Operand {
 };
 
 template <bool AR, bool BR, int WI, int WJ, int AF, int BF, bool DIRECT>
-__global__ __launch_bounds__(WI * WJ * 64) void product_kernel(const Args p) {
+__global__ __launch_bounds__(WI * WJ * 64, AF * BF == 64 ? 1 : 2) void product_kernel(const Args p) {
     constexpr int THREADS = WI * WJ * 64, TI = 16 * AF * WI, TJ = 16 * BF * WJ;
     typedef Operand<AR, TI, THREADS> OA;
     typedef Operand<BR, TJ, THREADS> OB;
@@ -295,7 +295,8 @@ __global__ __launch_bounds__(WI * WJ * 64) void product_kernel(const Args p) {
                                                  (int)(off_b[v] + (unsigned)((q - v) * OB::kLinesPer * p.ldb)), 0, 0, 0);
     };
     // through registers: a stage's pieces
-    uint4v ra[DIRECT ? 1 : OA::kPieces], rb[DIRECT ? 1 : OB::kPieces];
+    constexpr int AHEAD = DIRECT ? 1 : OA::kPieces + OB::kPieces <= 4 ? 4 : 2;
+    uint4v ra[AHEAD][DIRECT ? 1 : OA::kPieces], rb[AHEAD][DIRECT ? 1 : OB::kPieces];
     auto fetch = [&](auto tag, const unsigned char* at, long long ld, int rows, uint4v* regs) {
         typedef decltype(tag) O;
 #pragma unroll
@@ -307,19 +308,19 @@ __global__ __launch_bounds__(WI * WJ * 64) void product_kernel(const Args p) {
             if (line < lines && along > 0) regs[q] = load_part<DT>(reinterpret_cast<const T*>(at + line * ld) + piece * PER, along);
         }
     };
-    auto fetch_stage = [&] {
-        fetch(OA{}, pa, p.lda, p.I - now.i0, ra);
-        fetch(OB{}, pb, p.ldb, p.J - now.j0, rb);
+    auto fetch_stage = [&](int slot) {
+        fetch(OA{}, pa, p.lda, p.I - now.i0, ra[slot]);
+        fetch(OB{}, pb, p.ldb, p.J - now.j0, rb[slot]);
         pa += a_step;
         pb += b_step;
         c_left -= BK;
     };
-    auto put_stage = [&](int buf) {
+    auto put_stage = [&](int slot, int buf) {
         if constexpr (!DIRECT) {
 #pragma unroll
-            for (int q = 0; q < OA::kPieces; ++q) *reinterpret_cast<uint4v*>(lds + buf * OA::kBytes + (q * THREADS + t) * 16) = ra[q];
+            for (int q = 0; q < OA::kPieces; ++q) *reinterpret_cast<uint4v*>(lds + buf * OA::kBytes + (q * THREADS + t) * 16) = ra[slot][q];
 #pragma unroll
-            for (int q = 0; q < OB::kPieces; ++q) *reinterpret_cast<uint4v*>(lds + B_AT + buf * OB::kBytes + (q * THREADS + t) * 16) = rb[q];
+            for (int q = 0; q < OB::kPieces; ++q) *reinterpret_cast<uint4v*>(lds + B_AT + buf * OB::kBytes + (q * THREADS + t) * 16) = rb[slot][q];
         }
     };
 
@@ -530,27 +531,28 @@ __global__ __launch_bounds__(WI * WJ * 64) void product_kernel(const Args p) {
             pb = now.pb;
             c_left = now.c_left;
             clear();
-            fetch_stage();
-            put_stage(0);
-            for (int s = 0; s < now.stages; ++s) {
-                const int buf = s & 1;
-                __syncthreads();                   // stage s is in LDS for every wave, and no wave reads the other half any more
-                if (s + 1 < now.stages) fetch_stage();
-#pragma unroll
-                for (int k = 0; k < KS; ++k) {
-                    FragA fa;
-                    FragB fb;
-#pragma unroll
-                    for (int q = 0; q < AF + BF; ++q)
-                        read_one((lds_bytes)(lds + buf * OA::kBytes), (lds_bytes)(lds + B_AT + buf * OB::kBytes), k, q, fa, fb);
-#pragma unroll
-                    for (int m = 0; m < AF * BF; ++m) {
-                        acc[m / BF][m % BF] = mma(fb[m % BF], fa[m / BF], acc[m / BF][m % BF]);
-                        asm volatile("" : "+a"(acc[m / BF][m % BF]));
-                    }
-                }
-                if (s + 1 < now.stages) put_stage(buf ^ 1);
-            }
+            // (AHEAD stages are under way: a stage is short for a load from memory)
+            each<AHEAD>([&](auto d) { fetch_stage(d); });
+            put_stage(0, 0);
+            for (int s0 = 0; s0 < now.stages; s0 += AHEAD)
+                each<AHEAD>([&](auto d) {
+                    const int s = s0 + d, buf = s & 1;
+                    if (s >= now.stages) return;
+                    __syncthreads();               // stage s is in LDS for every wave, and no wave reads the other half any more
+                    fetch_stage(d);
+                    each<KS>([&](auto k) {
+                        FragA fa;
+                        FragB fb;
+                        each<AF + BF>([&](auto q) {
+                            read_one((lds_bytes)(lds + buf * OA::kBytes), (lds_bytes)(lds + B_AT + buf * OB::kBytes), k, q, fa, fb);
+                        });
+                        each<AF * BF>([&](auto m) {
+                            acc[m / BF][m % BF] = mma(fb[m % BF], fa[m / BF], acc[m / BF][m % BF]);
+                            asm volatile("" : "+a"(acc[m / BF][m % BF]));
+                        });
+                    });
+                    put_stage((d + 1) % AHEAD, buf ^ 1);
+                });
             finish(2 * OA::kBytes);
             __syncthreads();
         }
@@ -565,6 +567,7 @@ __global__ __launch_bounds__(256) void add_parts_kernel(const float* parts, int 
     if (i >= (unsigned long long)I) return;
     const int j = (int)(at % per_row) * 8, n = J - j;
     float v[1][8] = {}, w[8], bias[8];
+#pragma unroll 8
     for (int s = 0; s < splits; ++s) {
         load8<PCONV_F32>(parts + ((unsigned long long)s * I + i) * J + j, n, w);
 #pragma unroll
@@ -662,8 +665,8 @@ int add_parts(const Product& p, hipStream_t st) {
     return PCONV_OK;
 }
 
-template <bool AR, bool BR, int WI, int WJ, int AF, int BF>
-int launch_tile(const Product& p, bool direct, hipStream_t st) {
+template <bool AR, bool BR, bool DIRECT, int WI, int WJ, int AF, int BF>
+int launch_tile(const Product& p, hipStream_t st) {
     constexpr int TI = 16 * AF * WI, TJ = 16 * BF * WJ;
     Args a = make_args(p, TI, TJ);
     constexpr size_t lds = (3 * TI + 2 * TJ) * (size_t)kStageBytes;
@@ -672,15 +675,10 @@ int launch_tile(const Product& p, bool direct, hipStream_t st) {
     a.work = (unsigned)work;
     // as many workgroups as are resident, the same number on each XCD
     const unsigned grid = (unsigned)std::min<unsigned long long>((work + 7) / 8 * 8, kComputeUnits * (160 * 1024 / lds));
-#define PCONV_PRODUCT(DIRECT)                                                                                           \
-    {                                                                                                                   \
-        auto kern = product_kernel<AR, BR, WI, WJ, AF, BF, DIRECT>;                                                     \
-        static LdsAllowance allowed;                                                                                    \
-        if (lds > 64 * 1024) PCONV_HIP(allowed.ask((const void*)kern));                                                 \
-        hipLaunchKernelGGL(kern, dim3(grid), dim3(WI * WJ * 64), lds, st, a);                                 \
-    }
-    if (direct) PCONV_PRODUCT(true) else PCONV_PRODUCT(false)
-#undef PCONV_PRODUCT
+    auto kern = product_kernel<AR, BR, WI, WJ, AF, BF, DIRECT>;
+    static LdsAllowance allowed;
+    if (lds > 64 * 1024) PCONV_HIP(allowed.ask((const void*)kern));
+    hipLaunchKernelGGL(kern, dim3(grid), dim3(WI * WJ * 64), lds, st, a);
     PCONV_HIP(hipGetLastError());
     return add_parts(p, st);
 }
@@ -692,10 +690,17 @@ int launch_form(const Product& p, hipStream_t st) {
         return aligned_to(m, 16) && ld * ES % 16 == 0 && (rows || (long long)p.C * ES % 16 == 0);
     };
     const bool direct = fits(p.a, p.lda, AR) && fits(p.b, p.ldb, BR);
-    switch (p.tile) {
-        case 0: return launch_tile<AR, BR, 2, 2, 8, 8>(p, direct, st);
-        case 1: return launch_tile<AR, BR, 2, 2, 4, 4>(p, direct, st);
-        default: return launch_tile<AR, BR, 2, 2, 2, 2>(p, direct, st);
+    // (fp32: the matrix cores' rate is so low that the smallest tile feeds them, 2048^3: 131 us against 134 and 532 of the larger ones)
+    if constexpr (ES == 4)
+        return direct ? launch_tile<AR, BR, true, 2, 2, 2, 2>(p, st) : launch_tile<AR, BR, false, 2, 2, 2, 2>(p, st);
+    else {
+        // (through registers the largest tile has none left to look ahead)
+        if (!direct) return p.tile < 2 ? launch_tile<AR, BR, false, 2, 2, 4, 4>(p, st) : launch_tile<AR, BR, false, 2, 2, 2, 2>(p, st);
+        switch (p.tile) {
+            case 0: return launch_tile<AR, BR, true, 2, 2, 8, 8>(p, st);
+            case 1: return launch_tile<AR, BR, true, 2, 2, 4, 4>(p, st);
+            default: return launch_tile<AR, BR, true, 2, 2, 2, 2>(p, st);
+        }
     }
 }
 
