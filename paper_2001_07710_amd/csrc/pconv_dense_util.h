@@ -64,9 +64,13 @@ __device__ __forceinline__ uint4v load_part(const typename Store<DT>::T* p, int 
     constexpr int P = Store<DT>::kPer;
     if (n >= P) return load16(p);
     typename Store<DT>::V v = {};
+    if (n > 0) {                               // (one branch, and all of it under way at once)
+        typename Store<DT>::T each[P];
 #pragma unroll
-    for (int i = 0; i < P; ++i)
-        if (i < n) v[i] = p[i];
+        for (int i = 0; i < P; ++i) each[i] = p[i < n ? i : n - 1];
+#pragma unroll
+        for (int i = 0; i < P; ++i) v[i] = i < n ? each[i] : (typename Store<DT>::T)0.f;
+    }
     return __builtin_bit_cast(uint4v, v);
 }
 

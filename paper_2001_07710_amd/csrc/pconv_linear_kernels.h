@@ -297,20 +297,25 @@ __global__ __launch_bounds__(WI * WJ * 64, AF * BF == 64 ? 1 : 2) void product_k
     // through registers: a stage's pieces
     constexpr int AHEAD = DIRECT ? 1 : OA::kPieces + OB::kPieces <= 4 ? 4 : 2;
     uint4v ra[AHEAD][DIRECT ? 1 : OA::kPieces], rb[AHEAD][DIRECT ? 1 : OB::kPieces];
-    auto fetch = [&](auto tag, const unsigned char* at, long long ld, int rows, uint4v* regs) {
+    auto fetch = [&](auto tag, const unsigned char* at, unsigned long long left, long long ld, int rows, uint4v* regs) {
         typedef decltype(tag) O;
 #pragma unroll
         for (int q = 0; q < O::kPieces; ++q) {
             int line, piece;
             O::where(t, q, &line, &piece);
-            const int lines = O::kRows ? c_left : rows, along = (O::kRows ? rows : c_left) - piece * PER;
+            const int lines = O::kRows ? c_left : rows;
+            int along = (O::kRows ? rows : c_left) - piece * PER;
             regs[q] = uint4v{0, 0, 0, 0};
+            // (what stands behind the end of a line of i or j gives results that nobody stores: read whole, up to the matrix's end)
+            if (O::kRows && along > 0 && (unsigned long long)(line * ld) + piece * 16 + 16 <= left) along = PER;
             if (line < lines && along > 0) regs[q] = load_part<DT>(reinterpret_cast<const T*>(at + line * ld) + piece * PER, along);
         }
     };
     auto fetch_stage = [&](int slot) {
-        fetch(OA{}, pa, p.lda, p.I - now.i0, ra[slot]);
-        fetch(OB{}, pb, p.ldb, p.J - now.j0, rb[slot]);
+        fetch(OA{}, pa, a_left, p.lda, p.I - now.i0, ra[slot]);
+        fetch(OB{}, pb, b_left, p.ldb, p.J - now.j0, rb[slot]);
+        a_left -= a_step;
+        b_left -= b_step;
         pa += a_step;
         pb += b_step;
         c_left -= BK;
@@ -529,6 +534,8 @@ __global__ __launch_bounds__(WI * WJ * 64, AF * BF == 64 ? 1 : 2) void product_k
             now = work_at(id);
             pa = now.pa;
             pb = now.pb;
+            a_left = now.a_left;
+            b_left = now.b_left;
             c_left = now.c_left;
             clear();
             // (AHEAD stages are under way: a stage is short for a load from memory)
@@ -647,9 +654,14 @@ Args make_args(const Product& p, int tile_i, int tile_j) {
     a.C = p.C;
     a.c_per = p.c_per;
     const long long ra = p.a_rows ? p.C : p.I, la = p.a_rows ? p.I : p.C, rb = p.b_rows ? p.C : p.J, lb = p.b_rows ? p.J : p.C;
-    // (up to the end of the last element's 16 bytes, which lie in its page: a piece that begins inside is read whole)
-    a.a_span = ((unsigned long long)((ra - 1) * a.lda + la * ES) + 15) / 16 * 16;
-    a.b_span = ((unsigned long long)((rb - 1) * a.ldb + lb * ES) + 15) / 16 * 16;
+    // (of a matrix that begins at a multiple of 16 bytes, up to the end of the last element's 16, which lie in its page: a piece that
+    // begins inside is read whole)
+    auto span = [](const void* m, long long rows, long long ld, long long cols) {
+        const unsigned long long n = (unsigned long long)((rows - 1) * ld + cols * ES);
+        return aligned_to(m, 16) ? (n + 15) / 16 * 16 : n;
+    };
+    a.a_span = span(p.a, ra, a.lda, la);
+    a.b_span = span(p.b, rb, a.ldb, lb);
     a.tiles_i = (int)(((long long)p.I + tile_i - 1) / tile_i);
     a.tiles_j = (int)(((long long)p.J + tile_j - 1) / tile_j);
     a.f = p.f;
