@@ -187,6 +187,30 @@ __device__ __forceinline__ void times_slope8(float v[R][8], const float z[R][8],
 #undef PCONV_EACH
 }
 
+// out[j] of 64 columns from `first`, by a workgroup of 256: 16 threads to four columns, each with every 16th strip
+__device__ __forceinline__ void add_strips(const float* parts, int strips, int N, float* out, int first) {
+    __shared__ float sums[16][64];
+    const int c = threadIdx.x % 16 * 4, s = threadIdx.x / 16, j = first + c, n = N - j;
+    float sum[4] = {};
+    if (n > 0)
+#pragma unroll 4
+        for (int g = s; g < strips; g += 16) {
+            const float4v v = __builtin_bit_cast(float4v, load_part<PCONV_F32>(parts + (size_t)g * N + j, n));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] += v[e];
+        }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sums[s][c + e] = sum[e];
+    __syncthreads();
+    const int d = first + threadIdx.x;
+    if (threadIdx.x < 64 && d < N) {
+        float all = 0.f;
+#pragma unroll
+        for (int q = 0; q < 16; ++q) all += sums[q][threadIdx.x];
+        out[d] = all;
+    }
+}
+
 constexpr long long kMostStride = 1 << 20;
 
 inline bool is_dtype(int dtype) { return dtype == PCONV_F32 || dtype == PCONV_F16 || dtype == PCONV_BF16; }

@@ -20,6 +20,13 @@ struct Finish {
 };
 enum { kForward = 0, kGradInput = 1, kFloat = 2 };
 
+// Column sums that were taken over strips of rows and are still to be added: out[j] = sum of parts[strip][j].  parts null: none
+struct Strips {
+    const float* parts;
+    int strips, N;
+    float* out;
+};
+
 // R[i][j] = sum over c of A(i, c) * B(j, c).  A(i, c) is at a[i * lda + c] or, a_rows, at a[c * lda + i]; B alike.
 struct Product {
     const void* a;
@@ -31,6 +38,7 @@ struct Product {
     int tile;                   // kTiles index
     int splits, c_per;          // workgroups that share a tile, and the c each takes (a multiple of a stage's)
     float* parts;               // splits > 1: [splits][I][J] partial sums
+    Strips strips;              // added in the launch that adds the parts (splits > 1)
 };
 
 constexpr int kComputeUnits = 256;          // of an MI355X: plans and workspaces are the same whatever device is current

@@ -124,44 +124,20 @@ __global__ __launch_bounds__(256) void column_sums_kernel(const typename Store<D
         store8<PCONV_F32>(out + (size_t)blockIdx.y * N + j, n, sum);
     }
 }
-// 64 columns a workgroup, 16 threads to four of them, each with every 16th strip
-__global__ __launch_bounds__(256) void add_strips_kernel(const float* parts, int strips, int N, float* out) {
-    __shared__ float sums[16][64];
-    const int c = threadIdx.x % 16 * 4, s = threadIdx.x / 16, j = blockIdx.x * 64 + c, n = N - j;
-    float sum[4] = {};
-    if (n > 0)
-#pragma unroll 4
-        for (int g = s; g < strips; g += 16) {
-            const float4v v = __builtin_bit_cast(float4v, load_part<PCONV_F32>(parts + (size_t)g * N + j, n));
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sum[e] += v[e];
-        }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) sums[s][c + e] = sum[e];
-    __syncthreads();
-    const int d = blockIdx.x * 64 + threadIdx.x;
-    if (threadIdx.x < 64 && d < N) {
-        float all = 0.f;
-#pragma unroll
-        for (int q = 0; q < 16; ++q) all += sums[q][threadIdx.x];
-        out[d] = all;
-    }
-}
+__global__ __launch_bounds__(256) void add_strips_kernel(Strips s) { add_strips(s.parts, s.strips, s.N, s.out, blockIdx.x * 64); }
 __global__ __launch_bounds__(256) void fill_zero_kernel(float* out, unsigned long long n) {
     const unsigned long long i = (unsigned long long)blockIdx.x * 256 + threadIdx.x;
     if (i < n) out[i] = 0.f;
 }
 
+// Column sums of m, but for the adding of strips where there are several
 template <int DT>
-int column_sums(const void* m, long long ld, int M, int N, float* parts, float* out, hipStream_t st) {
+int column_sums(const void* m, long long ld, int M, int N, float* parts, float* out, Strips* left, hipStream_t st) {
     const int strips = sum_strips(M, N), per = (M + strips - 1) / strips;
     hipLaunchKernelGGL(column_sums_kernel<DT>, dim3((N + kSumCols - 1) / kSumCols, strips), dim3(256), 0, st,
                        static_cast<const typename Store<DT>::T*>(m), ld, M, N, per, strips > 1 ? parts : out);
     PCONV_HIP(hipGetLastError());
-    if (strips > 1) {
-        hipLaunchKernelGGL(add_strips_kernel, dim3((N + 63) / 64), dim3(256), 0, st, parts, strips, N, out);
-        PCONV_HIP(hipGetLastError());
-    }
+    if (strips > 1) *left = Strips{parts, strips, N, out};
     return PCONV_OK;
 }
 size_t strip_bytes(int M, int N) {
@@ -301,14 +277,18 @@ extern "C" int pconv_linear_grad_weight(const void* dz, long long lddz, const vo
     const Plan plan = plan_product(dtype, N, K, M, false);
     const size_t strips = strip_bytes(M, N);
     if (bad_workspace(workspace, workspace_bytes, strips + plan.part_bytes)) return PCONV_EINVAL;
+    Product p{};
     if (db) {
         float* const parts = static_cast<float*>(workspace);
-        int rc = dtype == PCONV_F32   ? column_sums<PCONV_F32>(dz, lddz, M, N, parts, db, st)
-                 : dtype == PCONV_F16 ? column_sums<PCONV_F16>(dz, lddz, M, N, parts, db, st)
-                                      : column_sums<PCONV_BF16>(dz, lddz, M, N, parts, db, st);
+        int rc = dtype == PCONV_F32   ? column_sums<PCONV_F32>(dz, lddz, M, N, parts, db, &p.strips, st)
+                 : dtype == PCONV_F16 ? column_sums<PCONV_F16>(dz, lddz, M, N, parts, db, &p.strips, st)
+                                      : column_sums<PCONV_BF16>(dz, lddz, M, N, parts, db, &p.strips, st);
         if (rc) return rc;
+        if (p.strips.parts && plan.splits == 1) {
+            hipLaunchKernelGGL(add_strips_kernel, dim3((N + 63) / 64), dim3(256), 0, st, p.strips);
+            PCONV_HIP(hipGetLastError());
+        }
     }
-    Product p{};
     p.a = dz; p.lda = lddz; p.b = x; p.ldb = ldx;
     p.I = N; p.J = K; p.C = M;
     p.a_rows = p.b_rows = true;

@@ -486,8 +486,10 @@ __global__ __launch_bounds__(WI * WJ * 64, AF * BF == 64 ? 1 : 2) void product_k
                 each<OA::kPieces>([&](auto q) { ask_a(into + s * OA::kBytes, q); });
                 each<OB::kPieces>([&](auto q) { ask_b(into + B_AT + s * OB::kBytes, q); });
             });
-            __builtin_amdgcn_s_waitcnt(0x0F70);                // vmcnt(0)
-            __syncthreads();
+            constexpr int PIECES = OA::kPieces + OB::kPieces;
+            __builtin_amdgcn_s_waitcnt(0x0F70 | (PIECES & 15) | (PIECES >> 4) << 14);      // vmcnt: all but the pieces of stage 1
+            meet();
+            int known = -1;                                    // the stage behind which this wave's pieces are known to be in LDS
             for (unsigned id = first; id < end; id += turn) {
                 const Work then = work_at(id + turn);
                 clear();
@@ -504,9 +506,8 @@ __global__ __launch_bounds__(WI * WJ * 64, AF * BF == 64 ? 1 : 2) void product_k
                     begin_stage();
                     __builtin_amdgcn_sched_barrier(0);
                     step(std::integral_constant<int, 0>{});
-                    // this wave's pieces of stage s + 1 are in LDS: all but those of A that were asked for just now; stage 1's have been
-                    // waited for
-                    asm volatile("s_cmp_eq_u32 %0, 0\n\ts_cbranch_scc1 .Lthere%=\n\ts_waitcnt vmcnt(%1)\n.Lthere%=:" : : "s"(s), "i"(OA::kPieces) : "scc", "memory");
+                    // this wave's pieces of stage s + 1 are in LDS: all but those of A that were asked for just now
+                    asm volatile("s_cmp_eq_u32 %0, %1\n\ts_cbranch_scc1 .Lthere%=\n\ts_waitcnt vmcnt(%2)\n.Lthere%=:" : : "s"(s), "s"(known), "i"(OA::kPieces) : "scc", "memory");
                     meet();                                    // so are the other waves', and all have read stage s
                     __builtin_amdgcn_sched_barrier(0);
                     step(std::integral_constant<int, 1>{});
@@ -521,6 +522,7 @@ __global__ __launch_bounds__(WI * WJ * 64, AF * BF == 64 ? 1 : 2) void product_k
                 }
                 // (vmcnt(0), here: the wait in stage 0 would be one for the results' stores too)
                 __builtin_amdgcn_s_waitcnt(0x0F70);
+                known = 0;
                 finish(a2);
                 meet();                                        // the windows are free again
                 now = then;
@@ -567,7 +569,12 @@ __global__ __launch_bounds__(WI * WJ * 64, AF * BF == 64 ? 1 : 2) void product_k
 }
 
 // The parts of a product that several workgroups share, added in their order, and its epilogue: eight results a thread.
-__global__ __launch_bounds__(256) void add_parts_kernel(const float* parts, int splits, int I, int J, Finish f) {
+// (The workgroups behind those add strips of column sums.)
+__global__ __launch_bounds__(256) void add_parts_kernel(const float* parts, int splits, int I, int J, Finish f, unsigned blocks, Strips strips) {
+    if (blockIdx.x >= blocks) {
+        add_strips(strips.parts, strips.strips, strips.N, strips.out, (int)(blockIdx.x - blocks) * 64);
+        return;
+    }
     const int per_row = (J + 7) / 8;
     const unsigned long long at = (unsigned long long)blockIdx.x * 256 + threadIdx.x;
     const unsigned long long i = at / per_row;
@@ -672,7 +679,8 @@ Args make_args(const Product& p, int tile_i, int tile_j) {
 int add_parts(const Product& p, hipStream_t st) {
     if (p.splits <= 1) return PCONV_OK;
     const unsigned long long threads = (unsigned long long)p.I * ((p.J + 7) / 8);
-    hipLaunchKernelGGL(add_parts_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, p.parts, p.splits, p.I, p.J, p.f);
+    const unsigned blocks = (unsigned)((threads + 255) / 256), more = p.strips.parts ? (unsigned)(p.strips.N + 63) / 64 : 0;
+    hipLaunchKernelGGL(add_parts_kernel, dim3(blocks + more), dim3(256), 0, st, p.parts, p.splits, p.I, p.J, p.f, blocks, p.strips);
     PCONV_HIP(hipGetLastError());
     return PCONV_OK;
 }
