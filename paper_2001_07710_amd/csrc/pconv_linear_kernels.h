@@ -393,7 +393,7 @@ __global__ __launch_bounds__(WI * WJ * 64, AF * BF == 64 ? 1 : 2) void product_k
         if (now.i0 + TI <= p.I && now.j0 + TJ <= p.J) {
             // A whole tile, with what it reads besides known to the compiler: loads in a branch, or none, would be waited for in front of
             // every window, and with them the stores of the window before.
-            auto whole = [&](auto kind, auto add, auto zin) {
+            [[maybe_unused]] auto whole = [&](auto kind, auto add, auto zin) {
                 f.kind = kind;
                 if constexpr (!add) f.add = nullptr;
                 if constexpr (!zin) f.zin = nullptr;
@@ -418,10 +418,31 @@ __global__ __launch_bounds__(WI * WJ * 64, AF * BF == 64 ? 1 : 2) void product_k
                     done();
                 }
             };
-            constexpr std::true_type yes{};
-            constexpr std::false_type no{};
-            if (f.kind == kFloat) whole(std::integral_constant<int, kFloat>{}, no, no);
-            else if constexpr (!BR) {
+            [[maybe_unused]] constexpr std::true_type yes{};
+            [[maybe_unused]] constexpr std::false_type no{};
+            if (f.kind == kFloat) {
+                // (floats leave as they are, 16 bytes a lane side by side)
+                float* const out = static_cast<float*>(f.out) + now.j0 + wj * 16 * BF + (lane % ROW_LANES) * 4;
+#pragma unroll 1
+                for (int a = 0; a < AF; ++a) {
+                    put(a);
+                    float4v v[TIMES][2];
+#pragma unroll
+                    for (int r = 0; r < TIMES; ++r)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const int row = lane / ROW_LANES + r * ROWS_AT_ONCE, q = lane % ROW_LANES + h * ROW_LANES;
+                            v[r][h] = *reinterpret_cast<const float4v*>(win + row * PITCH + (q ^ (row & SPREAD)) * 16);
+                        }
+#pragma unroll
+                    for (int r = 0; r < TIMES; ++r)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            store16(out + (long long)(i_first + a * 16 + r * ROWS_AT_ONCE) * f.ld_out + h * ROW_LANES * 4,
+                                    __builtin_bit_cast(uint4v, v[r][h]));
+                    done();
+                }
+            } else if constexpr (!BR) {
                 if (f.add) whole(std::integral_constant<int, kForward>{}, yes, no);
                 else whole(std::integral_constant<int, kForward>{}, no, no);
             } else if constexpr (!AR) {
