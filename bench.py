@@ -179,6 +179,8 @@ def main():
                     help="the nine VGG-16 shapes at batch 64 with channel-minor activations and outputs (PCONV_FLAG_NHWC)")
     ap.add_argument("--clustered", action="store_true",
                     help="VGG-16 shapes with clustered connectivity: filters in their own order against similarity order")
+    ap.add_argument("--dense", action="store_true",
+                    help="the dense half of VGG-16: norm, three fully connected layers and distillation, forward and backward")
     ap.add_argument("--layers", default="")
     ap.add_argument("--K", type=int, default=8)
     ap.add_argument("--keep", type=float, default=0.28)
@@ -216,6 +218,8 @@ def main():
         return backward_bench(args, torch, pc, L)
     if args.conv1x1:
         return conv1x1_bench(args, torch, pc, L)
+    if args.dense:
+        return dense_bench(args, torch, pc)
     if args.chain:
         return chain_bench(args, torch, pc, L)
     if args.layers:
@@ -879,6 +883,81 @@ def conv1x1_bench(args, torch, pc, L, brief=False):
            "layers": rows,
            "cpu_baseline": {"value": x1.shape[2] * x1.shape[3] * kept / el / 1e9, "unit": "effective GMAC/s", "cores": 1,
                             "kind": "oracle", "sample": f"{runs} runs of one image of {name}, {el * runs:.1f} s"}}
+    print(json.dumps(out), flush=True)
+
+
+def dense_bench(args, torch, pc):
+    """What VGG-16 has behind its pruned convolutions (include/pconv_dense.h), fp16 storage: the norm of the 512 x 7 x 7 features, three
+    fully connected layers (25088 -> 4096 -> 4096 -> 1000) and the distillation loss against a teacher's twenty best classes; inference
+    of one image, and one training step (forward and all gradients) at batch 64."""
+    g = torch.Generator(device="cuda").manual_seed(200107710)
+    st = torch.cuda.current_stream().cuda_stream
+    widths = [512 * 7 * 7, 4096, 4096, 1000]
+    acts = [pc.ACT_RELU, pc.ACT_RELU, pc.ACT_NONE]
+    new = lambda *shape: torch.empty(shape, dtype=torch.float16, device="cuda")  # noqa: E731
+    f32 = lambda *shape: torch.zeros(shape, device="cuda")  # noqa: E731
+    normal = lambda *shape: torch.randn(shape, generator=g, device="cuda")  # noqa: E731
+    w = [(normal(n, k) * (2.0 / k) ** 0.5).half() for k, n in zip(widths, widths[1:])]
+    b = [normal(n) * 0.1 for n in widths[1:]]
+    gamma, beta = f32(widths[0]) + 1.0, f32(widths[0])
+    scratch = lambda n: torch.empty(max(n, 16), dtype=torch.uint8, device="cuda")  # noqa: E731
+
+    def layers(M):
+        """(name, call, bytes that it cannot do without, floating point operations) of a batch of M, forward"""
+        x, h = normal(M, widths[0]).clamp(min=0).half(), [new(M, k) for k in widths]
+        mean, rstd = f32(M), f32(M)
+        steps = [("norm", lambda: pc.layer_norm(x, h[0], pc.F16, M, widths[0], gamma=gamma, beta=beta, mean=mean, rstd=rstd, stream=st),
+                  4.0 * M * widths[0], 0.0)]
+        for i, (k, n) in enumerate(zip(widths, widths[1:])):
+            need = pc.linear_workspace(pc.F16, M, n, k)
+            ws = scratch(need)
+            steps.append((f"fc{i + 6}", lambda i=i, k=k, n=n, ws=ws, need=need: pc.linear(
+                h[i], w[i], h[i + 1], pc.F16, M, n, k, bias=b[i], act=acts[i], workspace=ws, workspace_bytes=need, stream=st),
+                2.0 * (M * k + n * k + M * n), 2.0 * M * n * k))
+        return steps, x, h, mean, rstd
+
+    def backward(M, x, h, mean, rstd):
+        top = normal(M, 1000).topk(20, dim=1)
+        idx, val, loss, weight = top.indices.int(), top.values.contiguous(), f32(M), torch.full((M,), 1.0 / M, device="cuda")
+        d = [new(M, k) for k in widths]
+        steps = [("distill", lambda: pc.distill(h[3], idx, val, pc.F16, M, 1000, 20, 4.0, weight=weight, loss=loss, grad=d[3], stream=st),
+                  4.0 * M * 1000, 0.0)]
+        for i in (2, 1, 0):
+            k, n = widths[i], widths[i + 1]
+            n1, n2 = pc.linear_grad_input_workspace(pc.F16, M, n, k), pc.linear_grad_weight_workspace(pc.F16, M, n, k)
+            ws, dw, db = scratch(max(n1, n2)), f32(n, k), f32(n)
+            # (the layer in front ends in ReLU: its output stands for the argument)
+            steps.append((f"fc{i + 6}_grad_input", lambda i=i, k=k, n=n, ws=ws, n1=n1: pc.linear_grad_input(
+                d[i + 1], w[i], d[i], pc.F16, M, n, k, z=h[i] if i else None, act=pc.ACT_RELU if i else pc.ACT_NONE, workspace=ws,
+                workspace_bytes=n1, stream=st), 2.0 * (M * n + n * k + M * k * (2 if i else 1)), 2.0 * M * n * k))
+            steps.append((f"fc{i + 6}_grad_weight", lambda i=i, k=k, n=n, ws=ws, n2=n2, dw=dw, db=db: pc.linear_grad_weight(
+                d[i + 1], h[i], dw, pc.F16, M, n, k, db=db, workspace=ws, workspace_bytes=n2, stream=st),
+                2.0 * (M * n + M * k) + 4.0 * n * k, 2.0 * M * n * k))
+        need = pc.layer_norm_grad_workspace(pc.F16, M, widths[0])
+        ws, dx, dg, db = scratch(need), new(M, widths[0]), f32(widths[0]), f32(widths[0])
+        steps.append(("norm_grad", lambda: pc.layer_norm_grad(d[0], x, dx, mean, rstd, pc.F16, M, widths[0], gamma=gamma, dgamma=dg, dbeta=db,
+                                                              workspace=ws, workspace_bytes=need, stream=st), 6.0 * M * widths[0], 0.0))
+        return steps
+
+    def timed(steps):
+        rows = []
+        for name, call, nbytes, flops in steps:
+            _, ms = time_launches(torch, call, args.steps, args.warmup)
+            rows.append({"step": name, "us": ms * 1e3, "alg_GBs": nbytes / ms / 1e6, "TFLOPs": flops / ms / 1e9})
+            log(json.dumps(rows[-1]))
+        _, ms = time_launches(torch, lambda: [call() for _, call, _, _ in steps], args.steps, args.warmup)
+        return rows, ms, sum(s[2] for s in steps)
+
+    one, one_ms, one_bytes = timed(layers(1)[0])
+    forward, *kept = layers(64)
+    step, step_ms, step_bytes = timed(forward + backward(64, *kept))
+    out = {"metric": "algorithmic GB/s, training step of VGG-16's fully connected layers by distillation", "value": step_bytes / step_ms / 1e6,
+           "unit": "GB/s", "n_gpus": 1, "steps": args.steps, "warmup": args.warmup, "ms_per_step": step_ms, "higher_is_better": True,
+           "dtype": "f16 storage, f32 accumulate", "data": "synthetic",
+           "config": {"workload": "norm, 25088 -> 4096 -> 4096 -> 1000, distillation from 20 classes, batch 64, with all gradients"},
+           "roofline": {"bound": "hbm", "achieved": step_bytes / step_ms / 1e6, "peak": PEAK_HBM_GBS, "unit": "GB/s",
+                        "frac": step_bytes / step_ms / 1e6 / PEAK_HBM_GBS, "traffic": None, "kernel": "product_kernel"},
+           "inference_of_one_image": {"us": one_ms * 1e3, "alg_GBs": one_bytes / one_ms / 1e6, "steps": one}, "training_step": step}
     print(json.dumps(out), flush=True)
 
 

@@ -6,6 +6,8 @@
 // Workgroups walk over the rows, so that a thread's gamma and beta stay in registers too; in the backward pass so do its columns'
 // sums of dy * h and dy, which meet at the end: the threads with the same columns in LDS, the workgroups in the workspace.
 // Longer rows (than 1024 threads hold) are read twice or three times, from the caches.
+#include <type_traits>
+
 #include "pconv_dense_util.h"
 
 namespace pconv {
@@ -118,11 +120,9 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const NormArgs p) {
     const float inv = 1.f / (float)p.D;
     for (long long k = 0; k < turns; ++k) {
         const long long r0 = k * step * U + first;
-        // (the next rows are under way while these are worked on, where registers are left for them)
-        constexpr bool AHEAD = Q < 4;
-        if (!AHEAD && k) rows.load(p.x, p.ldx, r0, step, p.rows, p.D, t);
+        // (the next rows are under way while these are worked on)
         const Rows<DT, TPR, Q, U> now = rows;
-        if (AHEAD && k + 1 < turns) rows.load(p.x, p.ldx, r0 + step * U, step, p.rows, p.D, t);
+        if (k + 1 < turns) rows.load(p.x, p.ldx, r0 + step * U, step, p.rows, p.D, t);
         float mean[U], rstd[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -298,8 +298,24 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(const NormArgs p) {
     }
 }
 
-// Rows that no workgroup holds: one workgroup a row, in several readings.
+// Rows that no workgroup holds: one workgroup a row, in several readings, the first from memory.
 constexpr int kLong = 1024;
+// body(d, whole) for a thread's eights of a row's columns, from d on; whole: all eight are there
+template <typename F>
+__device__ __forceinline__ void along_row(int D, F body) {
+    int d = threadIdx.x * 8;
+#pragma unroll 4
+    for (; d + 8 <= D; d += kLong * 8) body(d, std::true_type{});
+    if (d < D) body(d, std::false_type{});
+}
+template <int DT, bool WHOLE>
+__device__ __forceinline__ void load_eight(const typename Store<DT>::T* p, int n, float (&v)[8]) {
+    Eight<DT> e;
+    if constexpr (WHOLE) e.load_whole(p);
+    else e.load(p, n);
+    e.get(v);
+}
+
 template <int DT>
 __global__ __launch_bounds__(kLong) void norm_long_kernel(const NormArgs p) {
     typedef typename Store<DT>::T T;
@@ -308,33 +324,36 @@ __global__ __launch_bounds__(kLong) void norm_long_kernel(const NormArgs p) {
     for (long long r = blockIdx.x; r < p.rows; r += gridDim.x) {
         const T* const x = static_cast<const T*>(p.x) + r * p.ldx;
         T* const y = static_cast<T*>(p.out) + r * p.ldo;
-        float sum[1] = {}, squares[1] = {}, v[8];
-        for (int d = threadIdx.x * 8; d < p.D; d += kLong * 8) {
-            load8<DT>(x + d, p.D - d, v);
+        float sum[1] = {}, squares[1] = {};
+        along_row(p.D, [&](int d, auto whole) {
+            float v[8];
+            load_eight<DT, whole>(x + d, p.D - d, v);
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum[0] += v[e];
-        }
+        });
         row_sum(sum);
         const float mean = sum[0] / (float)p.D;
-        for (int d = threadIdx.x * 8; d < p.D; d += kLong * 8) {
-            load8<DT>(x + d, p.D - d, v);
+        along_row(p.D, [&](int d, auto whole) {
+            float v[8];
+            load_eight<DT, whole>(x + d, p.D - d, v);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) squares[0] += d + e < p.D ? (v[e] - mean) * (v[e] - mean) : 0.f;
-        }
+            for (int e = 0; e < 8; ++e) squares[0] += whole || d + e < p.D ? (v[e] - mean) * (v[e] - mean) : 0.f;
+        });
         row_sum(squares);
         const float rstd = 1.f / sqrtf(squares[0] / (float)p.D + p.eps);
         if (threadIdx.x == 0) {
             if (p.mean) p.mean[r] = mean;
             if (p.rstd) p.rstd[r] = rstd;
         }
-        for (int d = threadIdx.x * 8; d < p.D; d += kLong * 8) {
-            const int n = p.D - d;
-            load8<DT>(x + d, n, v);
+        along_row(p.D, [&](int d, auto whole) {
+            float v[8], gamma[8], beta[8];
+            load_eight<DT, whole>(x + d, p.D - d, v);
+            load_columns(p.gamma, d, p.D, 1.f, 1.f, gamma);
+            load_columns(p.beta, d, p.D, 0.f, 0.f, beta);
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                v[e] = (v[e] - mean) * rstd * (p.gamma && e < n ? p.gamma[d + e] : 1.f) + (p.beta && e < n ? p.beta[d + e] : 0.f);
-            store8<DT>(y + d, n, v);
-        }
+            for (int e = 0; e < 8; ++e) v[e] = (v[e] - mean) * rstd * gamma[e] + beta[e];
+            store8<DT>(y + d, whole ? 8 : p.D - d, v);
+        });
     }
 }
 
@@ -348,30 +367,30 @@ __global__ __launch_bounds__(kLong) void norm_grad_long_kernel(const NormArgs p)
         const T* const dy = static_cast<const T*>(p.dy) + r * p.lddy;
         T* const dx = static_cast<T*>(p.out) + r * p.ldo;
         const float mean = p.mean[r], rstd = p.rstd[r];
-        float s[2] = {}, vx[8], vd[8];
-        for (int d = threadIdx.x * 8; d < p.D; d += kLong * 8) {
-            const int n = p.D - d;
-            load8<DT>(x + d, n, vx);
-            load8<DT>(dy + d, n, vd);
+        float s[2] = {};
+        along_row(p.D, [&](int d, auto whole) {
+            float vx[8], vd[8], gamma[8];
+            load_eight<DT, whole>(x + d, p.D - d, vx);
+            load_eight<DT, whole>(dy + d, p.D - d, vd);
+            load_columns(p.gamma, d, p.D, 1.f, 0.f, gamma);
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (e < n) {
-                    const float g = vd[e] * (p.gamma ? p.gamma[d + e] : 1.f);
-                    s[0] += g;
-                    s[1] += g * ((vx[e] - mean) * rstd);
-                }
-        }
+            for (int e = 0; e < 8; ++e) {
+                const float g = vd[e] * gamma[e];
+                s[0] += g;
+                s[1] += whole || d + e < p.D ? g * ((vx[e] - mean) * rstd) : 0.f;
+            }
+        });
         row_sum(s);
         const float s1 = s[0] / (float)p.D, s2 = s[1] / (float)p.D;
-        for (int d = threadIdx.x * 8; d < p.D; d += kLong * 8) {
-            const int n = p.D - d;
-            load8<DT>(x + d, n, vx);
-            load8<DT>(dy + d, n, vd);
+        along_row(p.D, [&](int d, auto whole) {
+            float vx[8], vd[8], gamma[8];
+            load_eight<DT, whole>(x + d, p.D - d, vx);
+            load_eight<DT, whole>(dy + d, p.D - d, vd);
+            load_columns(p.gamma, d, p.D, 1.f, 0.f, gamma);
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                vd[e] = rstd * (vd[e] * (p.gamma && e < n ? p.gamma[d + e] : 1.f) - s1 - (vx[e] - mean) * rstd * s2);
-            store8<DT>(dx + d, n, vd);
-        }
+            for (int e = 0; e < 8; ++e) vd[e] = rstd * (vd[e] * gamma[e] - s1 - (vx[e] - mean) * rstd * s2);
+            store8<DT>(dx + d, whole ? 8 : p.D - d, vd);
+        });
     }
 }
 
@@ -385,10 +404,19 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(const NormArgs p, int
     const int j = blockIdx.x * kSumCols + lane * 8, n = p.D - j;
     const long long r0 = (long long)blockIdx.y * per, r1 = min((long long)p.rows, r0 + per);
     float dg[8] = {}, db[8] = {}, vx[8], vd[8];
-    if (n > 0)
+    auto rows = [&](auto whole) {
+#pragma unroll 4
         for (long long r = r0 + wave; r < r1; r += 4) {
-            load8<DT>(static_cast<const T*>(p.x) + r * p.ldx + j, n, vx);
-            load8<DT>(static_cast<const T*>(p.dy) + r * p.lddy + j, n, vd);
+            Eight<DT> ex, ed;
+            if constexpr (whole) {
+                ex.load_whole(static_cast<const T*>(p.x) + r * p.ldx + j);
+                ed.load_whole(static_cast<const T*>(p.dy) + r * p.lddy + j);
+            } else {
+                ex.load(static_cast<const T*>(p.x) + r * p.ldx + j, n);
+                ed.load(static_cast<const T*>(p.dy) + r * p.lddy + j, n);
+            }
+            ex.get(vx);
+            ed.get(vd);
             const float mean = p.mean[r], rstd = p.rstd[r];
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
@@ -396,6 +424,9 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(const NormArgs p, int
                 db[q] += vd[q];
             }
         }
+    };
+    if (n >= 8) rows(std::true_type{});
+    else if (n > 0) rows(std::false_type{});
     if (wave) {
         store8<PCONV_F32>(&part[wave - 1][0][lane * 8], 8, dg);
         store8<PCONV_F32>(&part[wave - 1][1][lane * 8], 8, db);
@@ -466,10 +497,9 @@ Spread spread(int pieces) {
     if (pieces <= 512) return {256, 2, 1};
     if (pieces <= 1024) return {512, 2, 1};
     if (pieces <= 2048) return {1024, 2, 1};
-    if (pieces <= 4096) return {1024, 4, 1};
     return {0, 0, 1};
 }
-#define PCONV_SPREADS(X) X(8, 1, 4) X(16, 1, 4) X(32, 1, 4) X(64, 1, 4) X(64, 2, 2) X(256, 1, 2) X(256, 2, 1) X(512, 2, 1) X(1024, 2, 1) X(1024, 4, 1)
+#define PCONV_SPREADS(X) X(8, 1, 4) X(16, 1, 4) X(32, 1, 4) X(64, 1, 4) X(64, 2, 2) X(256, 1, 2) X(256, 2, 1) X(512, 2, 1) X(1024, 2, 1)
 // (the backward pass needs three times the registers)
 Spread grad_spread(int pieces) {
     if (pieces <= 8) return {8, 1, 2};
@@ -499,7 +529,7 @@ int grad_workgroups(const Spread& s, int rows) {
     const int groups = s.tpr ? backward_threads(s.tpr) / s.tpr : 1;
     return (int)std::min<long long>(((long long)rows + groups - 1) / groups, 256);
 }
-int strips(int rows, int D) { return std::max(1, std::min({64, (int)((rows + 63ll) / 64), 512 / ((D + kSumCols - 1) / kSumCols) + 1})); }
+int strips(int rows, int D) { return std::max(1, std::min({64, (int)((rows + 15ll) / 16), 512 / ((D + kSumCols - 1) / kSumCols) + 1})); }
 
 template <int DT>
 int launch_norm(const NormArgs& a, hipStream_t st) {
