@@ -134,10 +134,23 @@ constexpr float kLog2E = 1.44269504088896341f;
 
 __device__ __forceinline__ float relu(float z) { return z < 0.f ? 0.f : z; }                    // (NaN stays)
 __device__ __forceinline__ float relu_slope(float z) { return z > 0.f ? 1.f : z == z ? 0.f : z; }
-__device__ __forceinline__ float gelu(float z) { return z * (0.5f + 0.5f * erff(bounded(z) * kSqrtHalf)); }
+// Phi(t), the normal distribution, and e = exp(-t^2 / 2): Abramowitz and Stegun's 7.1.26 for erfc(|t| / sqrt(2)), off by 0.75e-7 of Phi at
+// most, without cancellation in the tail.  (erff added 25 % to a product of 8192 x 4096 x 4096, this 7 %.)
+__device__ __forceinline__ float normal_share(float t, float& e) {
+    const float k = __builtin_amdgcn_rcpf(fmaf(0.3275911f * kSqrtHalf, fabsf(t), 1.f));
+    e = __builtin_amdgcn_exp2f(-0.5f * kLog2E * t * t);
+    const float poly = k * fmaf(k, fmaf(k, fmaf(k, fmaf(k, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+    const float tail = 0.5f * poly * e;
+    return t < 0.f ? tail : 1.f - tail;
+}
+__device__ __forceinline__ float gelu(float z) {
+    float e;
+    return z * normal_share(bounded(z), e);
+}
 __device__ __forceinline__ float gelu_slope(float z) {
-    const float t = tamed(z);
-    return 0.5f + 0.5f * erff(t * kSqrtHalf) + t * kInvSqrt2Pi * __builtin_amdgcn_exp2f(-0.5f * kLog2E * t * t);
+    float e;
+    const float t = tamed(z), share = normal_share(t, e);
+    return fmaf(t * kInvSqrt2Pi, e, share);
 }
 // (1 + tanh(u)) / 2 = 1 / (1 + exp(-2u)): no cancellation where the curve nears 0
 __device__ __forceinline__ float gelu_tanh_share(float t) {

@@ -8,6 +8,8 @@
 // maximum and sum of a softmax in the first pass.  The entries are one wave's work, beside the reductions of the others; after the
 // row's w * T * q has been stored the entries' places are stored again with their p taken off, by the first entry of each index (for
 // all that share it).
+// 8192 x 32001, bf16, 64 entries: 219 us, 4.8 TB/s (a copy reaches 5.17).  With the entries in front of the row's loads, and every
+// exponential taken twice, it took 400.  256 x 1000: 6 us, the latency of the entries' and the row's loads and four reductions.
 #include "pconv_dense_util.h"
 
 namespace pconv {

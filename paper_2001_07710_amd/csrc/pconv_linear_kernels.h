@@ -3,18 +3,26 @@
 // R[i][j] = sum over c of A(i, c) * B(j, c), each operand stored with c along its rows ("c-minor": x and w of the forward
 // pass, dz of the input gradient) or across them ("rows": w of the input gradient, both operands of the weight gradient).
 //
-// A workgroup owns a tile of TI x TJ results and walks over c in stages of 128 bytes of a row (64 elements, 32 for fp32), two
-// stages in LDS: while one is multiplied the next is under way.
-//   c-minor operand: [row][8 pieces of 16 bytes]; piece p of a row lies at place p ^ swizzle(row), so that the 32 rows an
+// A workgroup of four waves owns a tile of TI x TJ results (256, 128 or 64 each way; a wave half of it each way) and walks over c in
+// stages of 128 bytes of a row (64 elements, 32 for fp32), three stages of A and two of B in LDS:
+//   c-minor operand: [row][8 pieces of 16 bytes]; piece p of a row lies at place p ^ swizzle(row), so that the 16 rows an
 //       operand read touches at one piece spread over the banks;
 //   rows operand:    [c][pieces of 16 bytes]; piece p lies at p ^ swizzle(c) likewise, and is read with
 //       ds_read_b64_tr_b16: four c of 16 rows a group of 16 lanes, handed over transposed (fp32: single words).
+// (No bank conflict is counted for any of the three forms.)
 // Where rows are aligned to 16 bytes the pieces go from memory to LDS without registers (buffer_load ... lds: a wave's 64
 // pieces land side by side, so the swizzle is applied to what each lane asks for); otherwise through registers.
 // Pieces outside the matrix are outside the buffer descriptor and read as zeros.
 //
 // The matrix instructions get B as their rows and A as their columns: a lane of the result then holds four consecutive j of one i.
-// They leave through a window of LDS that belongs to the wave, 32 i at a time, so that eight lanes store one 128-byte line.
+// They leave through a window of LDS that belongs to the wave, 16 i at a time, so that 16 lanes store 256 bytes of a row (of the
+// largest tile; through no window they would be pieces of 8 bytes).
+//
+// What bounds it.  Large products: the chip's power.  With fewer stalls a stage (2,570 clocks of which 2,048 are MFMAs on the largest tile)
+// the clock falls and the time stays: 1.4 to 2 GHz under these loops.  8192 x 4096 -> 16384, bf16: 780 us, 1.41 PFLOP/s, with z kept
+// and GELU 850; the library's plain product there 709.  Gradients of 8192 x 4096 -> 4096: input 220 us (1.25 PFLOP/s), weights 224.  Per
+// tile of 256 x 256 the results take 13,000 clocks, during which nothing is multiplied: a wave has its SIMD's registers to itself.
+// Small products: a launch, the latency of two stages, and the results' way out (512^3: 5.4 us).
 #include <type_traits>
 #include <utility>
 
@@ -403,9 +411,7 @@ __global__ __launch_bounds__(WI * WJ * 64, AF * BF == 64 ? 1 : 2) void product_k
 #pragma unroll
                         for (int r = 0; r < TIMES; ++r) next[r].template load_whole<add, zin>(f, i_first + a * 16 + r * ROWS_AT_ONCE, j);
                 };
-                load(0);
-#pragma unroll 1
-                for (int a = 0; a < AF; ++a) {
+                auto window = [&](int a) {
                     Beside beside[TIMES];
 #pragma unroll
                     for (int r = 0; r < TIMES; ++r) beside[r] = next[r];
@@ -416,7 +422,14 @@ __global__ __launch_bounds__(WI * WJ * 64, AF * BF == 64 ? 1 : 2) void product_k
                     for (int r = 0; r < TIMES; ++r) get(r, v[r]);
                     finish_rows<add, zin, TIMES>(f, v, bias, beside, i_first + a * 16, ROWS_AT_ONCE, j, 8);
                     done();
-                }
+                };
+                load(0);
+                // (the first one by itself: in front of the loop the same stores stand behind the loads as at its end, and a window's
+                // wait for its loads is none for the stores of the window before)
+                constexpr int PEELED = add || zin ? 1 : 0;
+                if constexpr (PEELED) window(0);
+#pragma unroll 1
+                for (int a = PEELED; a < AF; ++a) window(a);
             };
             [[maybe_unused]] constexpr std::true_type yes{};
             [[maybe_unused]] constexpr std::false_type no{};
@@ -614,7 +627,8 @@ __global__ __launch_bounds__(256) void add_parts_kernel(const float* parts, int 
 
 // Few rows of x (up to 16) with weights that are read once, straight into registers: memory bounds it, no operand is shared.  A
 // workgroup owns 16 rows of w; its waves take turns along k (a wave's 64 lanes: 16 rows x 4 pieces), and their sums meet in LDS
-// in the order of the waves.  v_mfma_f32_16x16x32: rows of the result are rows of w, its columns rows of x.
+// in the order of the waves.  Rows of the matrix instructions' results are rows of w, their columns rows of x: for one row fifteen
+// sixteenths of them are idle, and still far ahead of memory.  25088 -> 4096, fp16, one row: 38.5 us, 5.3 TB/s, what a copy reaches.
 constexpr int kFewWaves = 8;
 __global__ __launch_bounds__(kFewWaves * 64) void few_rows_kernel(const Args p) {
     __shared__ __align__(16) float sums[kFewWaves][16][20];

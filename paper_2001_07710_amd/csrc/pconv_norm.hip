@@ -3,9 +3,13 @@
 //
 // A row is held in registers by TPR threads, Q pieces of 16 bytes each, so that it is read once: mean, then the squares around
 // it (or, backward, the two sums of g and g * h), each a reduction over those threads by shuffles, across waves through LDS.
-// Workgroups walk over the rows, so that a thread's gamma and beta stay in registers too; in the backward pass so do its columns'
-// sums of dy * h and dy, which meet at the end: the threads with the same columns in LDS, the workgroups in the workspace.
+// Workgroups walk over the rows, several short ones at a time, the next ones under way while these are worked on, so that a
+// thread's gamma and beta stay in registers too; in the backward pass so do its columns' sums of dy * h and dy, which meet at the
+// end: the threads with the same columns in LDS, the workgroups in the workspace, one part for a compute unit, added in a second launch.
 // Longer rows (than 1024 threads hold) are read twice or three times, from the caches.
+// 16384 x 4096, bf16: forward 45 us (5.9 TB/s, part of it from the cache behind L2), backward 78 us with the column sums (5.2 TB/s; a
+// copy reaches 5.17).  200704 x 64, fp16: forward 14 us (3.6 TB/s), backward 20 (3.9): there a wave's row is one load of its
+// lanes, and the shuffles of eight rows at a time are a third of its instructions.
 #include <type_traits>
 
 #include "pconv_dense_util.h"
