@@ -185,6 +185,27 @@ def test_linear_gradients_are_exact_on_whole_numbers(dt, place):
     assert (db == 55.0).all()
 
 
+@pytest.mark.parametrize("place", [(0, 0), (8, 16), (3, 1)], ids=["tight", "gaps", "odd"])
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+def test_products_of_the_largest_tile_are_exact_on_whole_numbers(dt, place):
+    """Results x terms of each product: whole tiles, one for each workgroup; ragged ones, two for some; split along the contraction, the
+    last part shorter than the others."""
+    rng = np.random.default_rng(12)
+    for I, J, C in [(4096, 4096, 512), (4600, 6143, 300), (700, 1300, 16000)]:
+        say("largest tile", dt, place, I, J, C)
+        # sums stay below 6 * 16,000 + 80 < 2^24, and typical ones, 2 * sqrt(C), are told from their neighbours in either type
+        a, b, add = whole(rng, (I, C), 3), whole(rng, (J, C), 2), whole(rng, (I, J), 40)
+        bias = whole(rng, J, 30)
+        product = a @ b.T
+        y, z = _linear(a, b, dt, bias, add, "relu", True, *place)
+        zz = product + bias + add
+        assert np.array_equal(z, rounded(zz, dt)) and np.array_equal(y, rounded(np.maximum(zz, 0), dt)), (dt, place, I, J, C)
+        got = _grad_input(a, np.ascontiguousarray(b.T), dt, add, "relu", add, *place)
+        assert np.array_equal(got, rounded(np.where(add > 0, product, 0) + add, dt)), (dt, place, I, J, C)
+        dw, db = _grad_weight(np.ascontiguousarray(a.T), np.ascontiguousarray(b.T), dt, *place)
+        assert np.array_equal(dw, product) and np.array_equal(db, a.sum(1)), (dt, place, I, J, C)
+
+
 def _close(got, want, dt, slack):
     """|got - want| within the rounding of the stored result and `slack` for what 32-bit arithmetic before it may be off."""
     bound = HALF[dt] * np.abs(want) + TINY[dt] + slack * (1 + HALF[dt])
