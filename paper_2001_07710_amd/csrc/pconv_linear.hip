@@ -155,7 +155,7 @@ __global__ __launch_bounds__(256) void activation_grad_kernel(const typename Sto
     float v[1][8], a[1][8];
     load8<DT>(dy + i * lddy + j, n, v[0]);
     load8<DT>(z + i * ldz + j, n, a[0]);
-    times_slope8<1>(v, a, act);
+    times_slope8<DT, 1>(v, a, act);
     store8<DT>(dz + i * lddz + j, n, v[0]);
 }
 

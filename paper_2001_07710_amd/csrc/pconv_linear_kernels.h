@@ -132,7 +132,7 @@ __device__ __forceinline__ void finish_rows(const Finish& f, float v[R][8], cons
         if (f.z)
 #pragma unroll
             for (int r = 0; r < R; ++r) store8<DT>(static_cast<T*>(f.z) + (i + r * between) * f.ld_out + j, n, v[r]);
-        activate8<R>(v, f.act);
+        activate8<DT, R>(v, f.act);
         if (ADD && f.add && !f.first) plus();
     } else {
         if (ZIN && f.zin) {
@@ -140,7 +140,7 @@ __device__ __forceinline__ void finish_rows(const Finish& f, float v[R][8], cons
             for (int r = 0; r < R; ++r) {
                 float z[1][8];
                 beside[r].zin.get(z[0]);
-                times_slope8<1>(v + r, z, f.act);
+                times_slope8<DT, 1>(v + r, z, f.act);
             }
         }
         if (ADD && f.add) plus();

@@ -213,6 +213,18 @@ def _close(got, want, dt, slack):
     assert not bad.any(), (dt, int(bad.sum()), float(np.max((np.abs(got - want) / bound)[bad])))
 
 
+@pytest.mark.parametrize("dt", TYPES)
+def test_the_tail_of_gelu(dt):
+    """Relative to the tail itself: its curve to 20 units of 2^-24 with about as many for the evaluation (fp32: erfc to 16), the argument of
+    the exponential to t^2 / 2 * 2 units (t is rounded into it twice), one for each other product: (t^2 + 64) units."""
+    from math import erfc, sqrt
+    v = rounded(-np.linspace(0, 8, 3001), dt)[:, None]
+    y, z = _linear(v, np.ones((1, 1)), dt, None, None, "gelu", False, 0, 0)
+    assert np.array_equal(z, v)
+    want = v * np.vectorize(lambda t: erfc(-t / sqrt(2)) / 2)(v)
+    _close(y, want, dt, (v * v + 64) * U32 * np.abs(want))
+
+
 @pytest.mark.parametrize("act", D.ACTS)
 @pytest.mark.parametrize("dt", TYPES)
 def test_activations_and_their_slopes(dt, act):
