@@ -90,7 +90,7 @@ __global__ __launch_bounds__(THREADS, waves_per_simd(THREADS, Q)) void distill_k
     typedef typename Store<DT>::V Vec;
     constexpr int P = Store<DT>::kPer;
     __shared__ float room[2][16];
-    __shared__ float teacher[2];                           // largest t / T or NaN, sum of the exponentials
+    __shared__ float teacher[2];                           // largest t, sum of exp((t - largest) / T) or NaN
     extern __shared__ __align__(16) unsigned char entries[];
     const int k4 = (p.k + 3) / 4 * 4;
     int* const index = reinterpret_cast<int*>(entries);    // [k4], -1: not there
@@ -124,13 +124,14 @@ __global__ __launch_bounds__(THREADS, waves_per_simd(THREADS, Q)) void distill_k
         for (int q = 0; q < Q; ++q) raw[q] = load_piece<DT>(row, (t + q * THREADS) * P - shift, p.V);
     }
 
-    // the teacher's entries: the first wave's lanes, j = lane, lane + 64, ..
+    // the teacher's entries: the first wave's lanes, j = lane, lane + 64, ..  (t - largest before the division by T: t / T would round
+    // away what the logits differ by, and overflow where they are the type's lowest value)
     if (t < 64) {
         float top = -__builtin_inff(), some = 0.f, sum = 0.f;
         for (int j = lane; j < k4; j += 64) {
             const int i = j < p.k ? p.indices[r * p.k + j] : -1;
             const bool there = i >= 0 && i < p.V;
-            const float v = there ? p.values[r * p.k + j] * p.inv_t : -__builtin_inff();
+            const float v = there ? p.values[r * p.k + j] : -__builtin_inff();
             index[j] = there ? i : -1;
             prob[j] = v;
             top = fmaxf(top, v);
@@ -139,7 +140,7 @@ __global__ __launch_bounds__(THREADS, waves_per_simd(THREADS, Q)) void distill_k
         top = wave_reduce(top, larger);
         some = wave_reduce(some, larger);
         for (int j = lane; j < k4; j += 64)
-            if (index[j] >= 0) sum += __expf(prob[j] - top);
+            if (index[j] >= 0) sum += __expf((prob[j] - top) * p.inv_t);
         sum = wave_reduce(sum, plus);
         if (t == 0) {
             teacher[0] = top;
@@ -240,13 +241,13 @@ __global__ __launch_bounds__(THREADS, waves_per_simd(THREADS, Q)) void distill_k
             }
         }
     }
-    // the loss, and p in the place of t / T
+    // the loss, and p in the place of t
     if (t < 64) {
         const float log_total = logf(total), log_norm = logf(norm);
         float loss = 0.f;
         for (int j = lane; j < p.k; j += 64) {
             if (index[j] < 0) continue;
-            const float log_p = prob[j] - top - log_total, mine = __expf(log_p);
+            const float log_p = (prob[j] - top) * p.inv_t - log_total, mine = __expf(log_p);
             if (!(mine == 0.f)) loss += mine * (log_p - ((own[j] - largest) * p.inv_t - log_norm));
             prob[j] = mine;
         }

@@ -571,6 +571,33 @@ def test_distillation_of_extreme_logits(V):
     assert np.isnan(loss).all() and np.isnan(grad).all()
 
 
+def test_distillation_takes_the_teachers_logits_by_their_differences():
+    """A teacher's logits with a large one in common (whole numbers of quarters, so that the sums are exact) are the same teacher, and
+    entries that are all the type's lowest value are alike, not absent."""
+    rng = np.random.default_rng(33)
+    R, V, k, T = 7, 333, 20, float(np.float32(0.3))
+    s = rng.standard_normal((R, V)).astype(np.float32).astype(np.float64)
+    idx = np.stack([rng.permutation(V)[:k] for _ in range(R)]).astype(np.int32)
+    val = rng.integers(-8, 9, (R, k)) / 4.0
+    near = _distill(s, idx, val, "f32", T)
+    want_loss, want_grad = D.distill(s, idx, val, T)
+    bl, bg = _distill_bounds(s, idx, val, T, np.ones(R))
+    for far in (2.0 ** 20, -2.0 ** 20):
+        loss, grad = _distill(s, idx, val + far, "f32", T)[:2]
+        assert (np.abs(loss - want_loss) <= bl).all() and (np.abs(grad - want_grad) <= bg).all()
+        assert loss.tobytes() == near[0].tobytes() and grad.tobytes() == near[1].tobytes()
+    lowest = np.full((R, k), float(np.finfo(np.float32).min))
+    loss, grad = _distill(s, idx, lowest, "f32", T)[:2]
+    same_loss, same_grad = _distill(s, idx, np.zeros((R, k)), "f32", T)[:2]
+    assert loss.any() and loss.tobytes() == same_loss.tobytes() and grad.tobytes() == same_grad.tobytes()
+    lowest[:, 3] = 1.0                      # one entry has everything
+    loss, grad = _distill(s, idx, lowest, "f32", T)[:2]
+    alone = np.full((R, k), -np.inf)
+    alone[:, 3] = 1.0
+    same_loss, same_grad = _distill(s, idx, alone, "f32", T)[:2]
+    assert loss.tobytes() == same_loss.tobytes() and grad.tobytes() == same_grad.tobytes()
+
+
 # ------------------------------------------------------------------------------------------------------------------ together
 
 def _head_step(t, dt, st, scratch):
