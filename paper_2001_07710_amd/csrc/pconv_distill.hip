@@ -29,7 +29,18 @@ struct DistillArgs {
     long long ldl, ldg;
     int V, k;
     float inv_t, t;
+    float c, c_low;            // log2(e) / T, and what is missing to it
 };
+
+// exp(d / T) for d <= 0.  WIDE: to two units of 32 bits wherever d lies, the product's rounding and c's put right behind the exponential
+// (otherwise |d| / T units more: nothing that a gradient of 16 bits keeps).  d = -inf gives 0, NaN stays.
+template <bool WIDE>
+__device__ __forceinline__ float exp_over_t(float d, float c, float c_low) {
+    const float x = d * c, e = __builtin_amdgcn_exp2f(x);
+    if constexpr (!WIDE) return e;
+    const float rest = fmaf(d, c_low, fmaf(d, c, -x)) * 0.693147181f;
+    return fmaf(e, x < -200.f ? 0.f : rest, e);
+}
 
 template <typename F>
 __device__ __forceinline__ float wave_reduce(float v, F f) {
@@ -89,6 +100,7 @@ __global__ __launch_bounds__(THREADS, waves_per_simd(THREADS, Q)) void distill_k
     typedef typename Store<DT>::T T;
     typedef typename Store<DT>::V Vec;
     constexpr int P = Store<DT>::kPer;
+    constexpr bool WIDE = DT == PCONV_F32;
     __shared__ float room[2][16];
     __shared__ float teacher[2];                           // largest t, sum of exp((t - largest) / T) or NaN
     extern __shared__ __align__(16) unsigned char entries[];
@@ -140,7 +152,7 @@ __global__ __launch_bounds__(THREADS, waves_per_simd(THREADS, Q)) void distill_k
         top = wave_reduce(top, larger);
         some = wave_reduce(some, larger);
         for (int j = lane; j < k4; j += 64)
-            if (index[j] >= 0) sum += __expf((prob[j] - top) * p.inv_t);
+            if (index[j] >= 0) sum += exp_over_t<true>(prob[j] - top, p.c, p.c_low);
         sum = wave_reduce(sum, plus);
         if (t == 0) {
             teacher[0] = top;
@@ -149,7 +161,7 @@ __global__ __launch_bounds__(THREADS, waves_per_simd(THREADS, Q)) void distill_k
     }
 
     // the softmax of the row: largest, then the sum of u = exp((s - largest) / T)
-    const float c = p.inv_t * 1.44269504088896341f;
+    const float c = p.c, c_low = p.c_low;
     float u[Q ? Q : 1][P];
     float largest, norm = 0.f, m = -__builtin_inff();
     if (p.given) {
@@ -171,13 +183,13 @@ __global__ __launch_bounds__(THREADS, waves_per_simd(THREADS, Q)) void distill_k
 #pragma unroll
                 for (int e = 0; e < P; ++e) high = fmaxf(high, (float)v[e]);
                 if (high > m) {
-                    norm *= __builtin_amdgcn_exp2f((m - high) * c);
+                    norm *= exp_over_t<WIDE>(m - high, c, c_low);
                     m = high;
                 }
                 // (-inf adds nothing, also where all has been -inf so far)
 #pragma unroll
                 for (int e = 0; e < P; ++e)
-                    if (!((float)v[e] == -__builtin_inff())) norm += __builtin_amdgcn_exp2f(((float)v[e] - m) * c);
+                    if (!((float)v[e] == -__builtin_inff())) norm += exp_over_t<WIDE>((float)v[e] - m, c, c_low);
             }
         }
         largest = all_reduce<THREADS>(m, room[0], larger);
@@ -196,7 +208,7 @@ __global__ __launch_bounds__(THREADS, waves_per_simd(THREADS, Q)) void distill_k
         for (int q = 0; q < Q; ++q) {
             const Vec v = __builtin_bit_cast(Vec, raw[q]);
 #pragma unroll
-            for (int e = 0; e < P; ++e) u[q][e] = __builtin_amdgcn_exp2f(((float)v[e] - largest) * c);
+            for (int e = 0; e < P; ++e) u[q][e] = exp_over_t<WIDE>((float)v[e] - largest, c, c_low);
         }
     }
     if (!p.given) {
@@ -206,7 +218,7 @@ __global__ __launch_bounds__(THREADS, waves_per_simd(THREADS, Q)) void distill_k
 #pragma unroll
                 for (int e = 0; e < P; ++e) norm += u[q][e];
         } else {
-            if (m != largest) norm *= __builtin_amdgcn_exp2f((m - largest) * c);
+            if (m != largest) norm *= exp_over_t<WIDE>(m - largest, c, c_low);
             if (largest == -__builtin_inff()) norm = __builtin_nanf("");
         }
         norm = all_reduce<THREADS>(norm, room[1], plus);
@@ -236,7 +248,7 @@ __global__ __launch_bounds__(THREADS, waves_per_simd(THREADS, Q)) void distill_k
                 const Vec v = __builtin_bit_cast(Vec, load_piece<DT>(row, at, p.V));
                 float g[P];
 #pragma unroll
-                for (int e = 0; e < P; ++e) g[e] = each * __builtin_amdgcn_exp2f(((float)v[e] - largest) * c);
+                for (int e = 0; e < P; ++e) g[e] = each * exp_over_t<WIDE>((float)v[e] - largest, c, c_low);
                 store_piece<DT>(out, at, p.V, g);
             }
         }
@@ -247,7 +259,7 @@ __global__ __launch_bounds__(THREADS, waves_per_simd(THREADS, Q)) void distill_k
         float loss = 0.f;
         for (int j = lane; j < p.k; j += 64) {
             if (index[j] < 0) continue;
-            const float log_p = (prob[j] - top) * p.inv_t - log_total, mine = __expf(log_p);
+            const float d = prob[j] - top, log_p = d * p.inv_t - log_total, mine = exp_over_t<true>(d, c, c_low) / total;
             if (!(mine == 0.f)) loss += mine * (log_p - ((own[j] - largest) * p.inv_t - log_norm));
             prob[j] = mine;
         }
@@ -272,7 +284,7 @@ __global__ __launch_bounds__(THREADS, waves_per_simd(THREADS, Q)) void distill_k
                     if (o < j) first = false;
                     else mine += prob[o];
                 }
-        if (first) out[i] = (T)(each * __builtin_amdgcn_exp2f((own[j] - largest) * c) - scale * mine);
+        if (first) out[i] = (T)(each * exp_over_t<WIDE>(own[j] - largest, c, c_low) - scale * mine);
     }
 }
 
@@ -316,6 +328,8 @@ int distill(const void* logits, long long ldl, const int32_t* indices, const flo
     a.given = given; a.stats = stats;
     a.V = V; a.k = k;
     a.t = temperature; a.inv_t = 1.f / temperature;
+    const double c = 1.4426950408889634 / (double)temperature;
+    a.c = (float)c; a.c_low = (float)(c - (double)a.c);
     hipStream_t st = static_cast<hipStream_t>(stream);
     return dtype == PCONV_F32   ? launch_distill<PCONV_F32>(a, R, st)
            : dtype == PCONV_F16 ? launch_distill<PCONV_F16>(a, R, st)

@@ -598,6 +598,21 @@ def test_distillation_takes_the_teachers_logits_by_their_differences():
     assert loss.tobytes() == same_loss.tobytes() and grad.tobytes() == same_grad.tobytes()
 
 
+def test_small_probabilities_are_as_exact_as_large_ones_in_32_bits():
+    """Logits of whole 2^-10, whose differences are exact, down to 60 T below the largest.  In units of 2^-24: the sum of 400 exponentials
+    in 14 additions on top of each other 14, its exponentials 4, the element's exponential 4, two products and two quotients 4: 26, with
+    the second-order terms 28."""
+    rng = np.random.default_rng(34)
+    R, V, T = 8, 400, 0.25
+    s = -rng.integers(0, 15 * 1024, (R, V)) / 1024.0
+    s[:, 17] = 0.0
+    _, grad = _distill(s, np.full((R, 1), 17, np.int32), np.zeros((R, 1)), "f32", T)[:2]
+    q = np.exp(s / T)
+    q /= q.sum(1, keepdims=True)
+    others = np.arange(V) != 17
+    assert (np.abs(grad[:, others] - T * q[:, others]) <= 28 * U32 * T * q[:, others]).all()
+
+
 # ------------------------------------------------------------------------------------------------------------------ together
 
 def _head_step(t, dt, st, scratch):
