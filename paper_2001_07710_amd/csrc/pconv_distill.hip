@@ -289,20 +289,34 @@ __global__ __launch_bounds__(THREADS, waves_per_simd(THREADS, Q)) void distill_k
 }
 
 template <int DT>
-int launch_distill(const DistillArgs& a, int R, hipStream_t st) {
+int launch_distill(DistillArgs a, int R, hipStream_t st) {
+    typedef typename Store<DT>::T T;
     constexpr int P = Store<DT>::kPer;
+    // (a launch holds fewer than 2^32 threads)
+    constexpr int kMostAtOnce = 1 << 21;
     const int pieces = a.V / P + 2;                    // (of a row that begins anywhere)
     const size_t lds = 3 * (size_t)((a.k + 3) / 4 * 4) * 4;
-#define PCONV_ROWS(THREADS, Q)                                                                                   \
-    if (!done && pieces <= THREADS * Q) {                                                                        \
-        hipLaunchKernelGGL((distill_kernel<DT, THREADS, Q>), dim3((unsigned)R), dim3(THREADS), lds, st, a);      \
-        done = true;                                                                                             \
+    for (int rows; R > 0; R -= rows) {
+        rows = std::min(R, kMostAtOnce);
+#define PCONV_ROWS(THREADS, Q)                                                                                      \
+    if (!done && pieces <= THREADS * Q) {                                                                           \
+        hipLaunchKernelGGL((distill_kernel<DT, THREADS, Q>), dim3((unsigned)rows), dim3(THREADS), lds, st, a);      \
+        done = true;                                                                                                \
     }
-    bool done = false;
-    PCONV_ROWS(64, 2) PCONV_ROWS(256, 2) PCONV_ROWS(256, 4) PCONV_ROWS(1024, 2) PCONV_ROWS(1024, 4) PCONV_ROWS(1024, 8)
-    if (!done) hipLaunchKernelGGL((distill_kernel<DT, 1024, 0>), dim3((unsigned)R), dim3(1024), lds, st, a);
+        bool done = false;
+        PCONV_ROWS(64, 2) PCONV_ROWS(256, 2) PCONV_ROWS(256, 4) PCONV_ROWS(1024, 2) PCONV_ROWS(1024, 4) PCONV_ROWS(1024, 8)
+        if (!done) hipLaunchKernelGGL((distill_kernel<DT, 1024, 0>), dim3((unsigned)rows), dim3(1024), lds, st, a);
 #undef PCONV_ROWS
-    PCONV_HIP(hipGetLastError());
+        PCONV_HIP(hipGetLastError());
+        a.logits = static_cast<const T*>(a.logits) + rows * a.ldl;
+        a.indices += (long long)rows * a.k;
+        a.values += (long long)rows * a.k;
+        if (a.weight) a.weight += rows;
+        if (a.loss) a.loss += rows;
+        if (a.grad) a.grad = static_cast<T*>(a.grad) + rows * a.ldg;
+        if (a.given) a.given += 2 * (long long)rows;
+        if (a.stats) a.stats += 2 * (long long)rows;
+    }
     return PCONV_OK;
 }
 

@@ -125,9 +125,18 @@ __global__ __launch_bounds__(256) void column_sums_kernel(const typename Store<D
     }
 }
 __global__ __launch_bounds__(256) void add_strips_kernel(Strips s) { add_strips(s.parts, s.strips, s.N, s.out, blockIdx.x * 64); }
-__global__ __launch_bounds__(256) void fill_zero_kernel(float* out, unsigned long long n) {
-    const unsigned long long i = (unsigned long long)blockIdx.x * 256 + threadIdx.x;
+constexpr unsigned kMostThreads = 1u << 28;     // of the launches of one thread for each piece (HIP takes fewer than 2^32)
+__global__ __launch_bounds__(256) void fill_zero_kernel(float* out, unsigned n) {
+    const unsigned i = blockIdx.x * 256 + threadIdx.x;
     if (i < n) out[i] = 0.f;
+}
+int fill_zero(float* out, unsigned long long n, hipStream_t st) {
+    for (unsigned now; n > 0; n -= now, out += now) {
+        now = (unsigned)std::min<unsigned long long>(n, kMostThreads);
+        hipLaunchKernelGGL(fill_zero_kernel, dim3((now + 255) / 256), dim3(256), 0, st, out, now);
+        PCONV_HIP(hipGetLastError());
+    }
+    return PCONV_OK;
 }
 
 // Column sums of m, but for the adding of strips where there are several
@@ -148,9 +157,9 @@ size_t strip_bytes(int M, int N) {
 template <int DT>
 __global__ __launch_bounds__(256) void activation_grad_kernel(const typename Store<DT>::T* dy, long long lddy, const typename Store<DT>::T* z,
                                                               long long ldz, typename Store<DT>::T* dz, long long lddz, int M, int N, int act) {
-    const unsigned per_row = (unsigned)(N + 7) / 8;
-    const unsigned long long at = (unsigned long long)blockIdx.x * 256 + threadIdx.x, i = at / per_row;
-    if (i >= (unsigned long long)M) return;
+    const unsigned per_row = (unsigned)(N + 7) / 8, at = blockIdx.x * 256 + threadIdx.x;
+    const long long i = at / per_row;
+    if (i >= M) return;
     const int j = (int)(at % per_row) * 8, n = N - j;
     float v[1][8], a[1][8];
     load8<DT>(dy + i * lddy + j, n, v[0]);
@@ -162,11 +171,18 @@ __global__ __launch_bounds__(256) void activation_grad_kernel(const typename Sto
 template <int DT>
 int activation_grad(const void* dy, long long lddy, const void* z, long long ldz, void* dz, long long lddz, int M, int N, int act, hipStream_t st) {
     typedef typename Store<DT>::T T;
-    const unsigned long long blocks = ((unsigned long long)M * ((N + 7ll) / 8) + 255) / 256;
-    if (blocks > 0x7FFFFFFFull) return PCONV_EUNSUPPORTED;
-    hipLaunchKernelGGL(activation_grad_kernel<DT>, dim3((unsigned)blocks), dim3(256), 0, st, static_cast<const T*>(dy), lddy,
-                       static_cast<const T*>(z), ldz, static_cast<T*>(dz), lddz, M, N, act);
-    PCONV_HIP(hipGetLastError());
+    const T *gradient = static_cast<const T*>(dy), *argument = static_cast<const T*>(z);
+    T* out = static_cast<T*>(dz);
+    const int per_row = (N + 7) / 8, most = (int)(kMostThreads / per_row);
+    for (int rows; M > 0; M -= rows) {
+        rows = std::min(M, most);
+        hipLaunchKernelGGL(activation_grad_kernel<DT>, dim3((unsigned)(((long long)rows * per_row + 255) / 256)), dim3(256), 0, st, gradient, lddy,
+                           argument, ldz, out, lddz, rows, N, act);
+        PCONV_HIP(hipGetLastError());
+        gradient += rows * lddy;
+        argument += rows * ldz;
+        out += rows * lddz;
+    }
     return PCONV_OK;
 }
 
@@ -261,15 +277,8 @@ extern "C" int pconv_linear_grad_weight(const void* dz, long long lddz, const vo
     if (!dw || !aligned_to(dw, 4) || !aligned_to(db, 4)) return PCONV_EINVAL;
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (M == 0) {
-        const unsigned long long n = (unsigned long long)N * K;
-        if ((n + 255) / 256 > 0x7FFFFFFFull) return PCONV_EUNSUPPORTED;
-        hipLaunchKernelGGL(fill_zero_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, dw, n);
-        PCONV_HIP(hipGetLastError());
-        if (db) {
-            hipLaunchKernelGGL(fill_zero_kernel, dim3((N + 255) / 256), dim3(256), 0, st, db, (unsigned long long)N);
-            PCONV_HIP(hipGetLastError());
-        }
-        return PCONV_OK;
+        if (int rc = fill_zero(dw, (unsigned long long)N * K, st)) return rc;
+        return db ? fill_zero(db, N, st) : PCONV_OK;
     }
     if (!dz || !x) return PCONV_EINVAL;
     for (const void* p : {dz, x})

@@ -613,6 +613,55 @@ def test_small_probabilities_are_as_exact_as_large_ones_in_32_bits():
     assert (np.abs(grad[:, others] - T * q[:, others]) <= 28 * U32 * T * q[:, others]).all()
 
 
+def test_distillation_of_more_rows_than_a_launch_takes():
+    """2^26 rows of 64 threads are as many threads as no launch has."""
+    import torch
+    R, T = (1 << 26) + 5, 2.0
+    g = torch.Generator(device="cuda").manual_seed(5)
+    s = torch.randn(R, 2, generator=g, device="cuda").half()
+    idx = torch.randint(0, 2, (R, 1), generator=g, device="cuda", dtype=torch.int32)
+    val = torch.zeros(R, 1, device="cuda")
+    loss, grad, stats = torch.full((R,), 55.0, device="cuda"), torch.full_like(s, 55.0), torch.full((R, 2), 55.0, device="cuda")
+    say("distill", R)
+    pc.distill(s, idx, val, pc.F16, R, 2, 1, T, loss=loss, grad=grad, stats=stats, stream=stream())
+    again = torch.full_like(grad, 55.0)
+    pc.distill_grad(s, idx, val, stats, again, pc.F16, R, 2, 1, T, stream=stream())
+    torch.cuda.synchronize()
+    assert bool((again == grad).all())
+    for at in range(0, R, 1 << 24):
+        part = slice(at, at + (1 << 24))
+        x, i = s[part].double(), idx[part].long()
+        far = (x.gather(1, 1 - i) - x.gather(1, i))[:, 0] / T       # the other logit's distance: log q = -log(1 + exp(far))
+        want = T * T * torch.log1p(torch.exp(far))
+        # (the largest logit's own exponential is 1: the loss is off by units of log(norm) and of the distance, 6 units of 1 + |far| each)
+        assert bool(((loss[part].double() - want).abs() <= T * T * 12 * U32 * (1 + far.abs())).all())
+        q = 1 / (1 + torch.exp(far))
+        own, other = grad[part].double().gather(1, i)[:, 0], grad[part].double().gather(1, 1 - i)[:, 0]
+        for have, right in ((own, T * (q - 1)), (other, T * (1 - q))):
+            # half a step of fp16, and 16 units of 32 bits of the terms, T at most
+            assert bool(((have - right).abs() <= HALF["f16"] * right.abs() + TINY["f16"] + 16 * U32 * T * (1 + far.abs())).all())
+
+
+def test_elementwise_passes_of_more_pieces_than_a_launch_takes():
+    """Rows of one element, 2^28 to a launch, and a weight gradient of more floats than that."""
+    import torch
+    M = (1 << 28) + 3
+    z = torch.ones(M, dtype=torch.bfloat16, device="cuda")
+    z[1::2] = -1
+    dz = torch.full_like(z, 3.0)
+    say("activation_grad", M)
+    pc.activation_grad(dz, z, dz, pc.BF16, M, 1, pc.ACT_RELU, stream=stream())
+    torch.cuda.synchronize()
+    assert bool((dz[0::2] == 3).all()) and not bool(dz[1::2].any())
+    del z, dz
+    N, K = (1 << 14) + 1, 1 << 14
+    dw, db = torch.full((N * K + 64,), 55.0, device="cuda"), torch.full((N + 64,), 55.0, device="cuda")
+    say("grad_weight of no rows", N, K)
+    pc.linear_grad_weight(None, None, dw, pc.F16, 0, N, K, db=db, stream=stream())
+    torch.cuda.synchronize()
+    assert not bool(dw[:N * K].any()) and bool((dw[N * K:] == 55).all()) and not bool(db[:N].any()) and bool((db[N:] == 55).all())
+
+
 # ------------------------------------------------------------------------------------------------------------------ together
 
 def _head_step(t, dt, st, scratch):
