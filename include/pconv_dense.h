@@ -39,6 +39,7 @@ enum { PCONV_ACT_NONE = 0,
        PCONV_ACT_GELU = 2,       /* z * Phi(z), Phi the normal distribution */
        PCONV_ACT_GELU_TANH = 3,  /* z/2 * (1 + tanh(sqrt(2/pi) * (z + 0.044715 z^3))) */
        PCONV_ACT_SILU = 4        /* z / (1 + exp(-z)) */ };
+/* (At z = -inf the last three are NaN, like the formulas; their slopes there are 0.) */
 
 enum { PCONV_FLAG_RESIDUAL_FIRST = 8u };   /* pconv_linear: the residual is added in front of the activation */
 

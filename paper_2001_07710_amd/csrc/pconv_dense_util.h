@@ -124,7 +124,7 @@ __device__ __forceinline__ void store8(typename Store<DT>::T* p, int n, const fl
 
 constexpr float kSqrtHalf = 0.70710678118654752f, kSqrt2OverPi = 0.79788456080286536f, kInvSqrt2Pi = 0.39894228040143268f;
 
-// z moved into +-100: behind that an activation's curve is 0 or 1 (times z) in 32 bits, and no inf * 0 arises.  `tamed` leaves NaN as it
+// z moved into +-100: behind that an activation's curve is 0 or 1 (times z) in 32 bits, and its slope meets no inf * 0.  `tamed` leaves NaN as it
 // is; `bounded`, one instruction, does not: for curves, which z itself multiplies.
 __device__ __forceinline__ float tamed(float z) { return z > 100.f ? 100.f : z < -100.f ? -100.f : z; }
 __device__ __forceinline__ float bounded(float z) { return __builtin_amdgcn_fmed3f(z, -100.f, 100.f); }

@@ -3,13 +3,15 @@
 // once, the gradient out once.
 //
 // One workgroup per row.  The row's logits are read once, Q pieces of 16 bytes a thread, and stay in registers, first as they are
-// stored, then as their exponentials: largest, sum of the exponentials, gradient.  (A row begins at any element: pieces are those
-// of memory, cut at the row's ends, so that every access is aligned.)  Longer rows are read again for the gradient, with the running
-// maximum and sum of a softmax in the first pass.  The entries are one wave's work, beside the reductions of the others; after the
-// row's w * T * q has been stored the entries' places are stored again with their p taken off, by the first entry of each index (for
-// all that share it).
+// stored, then, up to eight pieces, as their exponentials: largest, sum of the exponentials, gradient.  (A row begins at any element:
+// pieces are those of memory, cut at the row's ends, so that every access is aligned.)  Longer rows are read again for the gradient,
+// with the running maximum and sum of a softmax in the first pass.  The entries are one wave's work, beside the reductions of the
+// others; after the row's w * T * q has been stored the entries' places are stored again with their p taken off, by the first entry of
+// each index (for all that share it).
 // 8192 x 32001, bf16, 64 entries: 219 us, 4.8 TB/s (a copy reaches 5.17).  With the entries in front of the row's loads, and every
-// exponential taken twice, it took 400.  256 x 1000: 6 us, the latency of the entries' and the row's loads and four reductions.
+// exponential taken twice, it took 400.  4096 x 128000: 488 us, 4.3 TB/s (4.0 with the row read again; one workgroup fills a compute
+// unit there, and the exponentials are taken twice).  256 x 1000: 6 us, the latency of the entries' and the row's loads and four
+// reductions.  Few rows of many logits are a compute unit's work each: one of 128,000 takes 20 us.
 #include "pconv_dense_util.h"
 
 namespace pconv {
@@ -162,7 +164,9 @@ __global__ __launch_bounds__(THREADS, waves_per_simd(THREADS, Q)) void distill_k
 
     // the softmax of the row: largest, then the sum of u = exp((s - largest) / T)
     const float c = p.c, c_low = p.c_low;
-    float u[Q ? Q : 1][P];
+    // the exponentials are kept where the registers hold them beside the row (16 pieces: they are taken twice)
+    constexpr bool KEEP = Q > 0 && Q <= 8;
+    float u[KEEP ? Q : 1][P];
     float largest, norm = 0.f, m = -__builtin_inff();
     if (p.given) {
         largest = p.given[2 * r];
@@ -202,7 +206,7 @@ __global__ __launch_bounds__(THREADS, waves_per_simd(THREADS, Q)) void distill_k
     // the row's own logits at the entries, before any of the gradient is stored: grad may be logits
     if (t < 64)
         for (int j = lane; j < p.k; j += 64) own[j] = index[j] >= 0 ? (float)row[index[j]] : 0.f;
-    if constexpr (Q > 0) {
+    if constexpr (KEEP) {
         // (what lies outside the row is -inf: nothing, or NaN where the row is all -inf)
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
@@ -214,9 +218,14 @@ __global__ __launch_bounds__(THREADS, waves_per_simd(THREADS, Q)) void distill_k
     if (!p.given) {
         if constexpr (Q > 0) {
 #pragma unroll
-            for (int q = 0; q < Q; ++q)
+            for (int q = 0; q < Q; ++q) {
+                [[maybe_unused]] const Vec v = __builtin_bit_cast(Vec, raw[q]);
 #pragma unroll
-                for (int e = 0; e < P; ++e) norm += u[q][e];
+                for (int e = 0; e < P; ++e) {
+                    if constexpr (KEEP) norm += u[q][e];
+                    else norm += exp_over_t<WIDE>((float)v[e] - largest, c, c_low);
+                }
+            }
         } else {
             if (m != largest) norm *= exp_over_t<WIDE>(m - largest, c, c_low);
             if (largest == -__builtin_inff()) norm = __builtin_nanf("");
@@ -237,9 +246,13 @@ __global__ __launch_bounds__(THREADS, waves_per_simd(THREADS, Q)) void distill_k
 #pragma unroll
             for (int q = 0; q < Q; ++q) {
                 const int at = (t + q * THREADS) * P - shift;
+                [[maybe_unused]] const Vec v = __builtin_bit_cast(Vec, raw[q]);
                 float g[P];
 #pragma unroll
-                for (int e = 0; e < P; ++e) g[e] = each * u[q][e];
+                for (int e = 0; e < P; ++e) {
+                    if constexpr (KEEP) g[e] = each * u[q][e];
+                    else g[e] = each * exp_over_t<WIDE>((float)v[e] - largest, c, c_low);
+                }
                 if (at < p.V) store_piece<DT>(out, at, p.V, g);
             }
         } else {
@@ -304,7 +317,7 @@ int launch_distill(DistillArgs a, int R, hipStream_t st) {
         done = true;                                                                                                \
     }
         bool done = false;
-        PCONV_ROWS(64, 2) PCONV_ROWS(256, 2) PCONV_ROWS(256, 4) PCONV_ROWS(1024, 2) PCONV_ROWS(1024, 4) PCONV_ROWS(1024, 8)
+        PCONV_ROWS(64, 2) PCONV_ROWS(256, 2) PCONV_ROWS(256, 4) PCONV_ROWS(1024, 2) PCONV_ROWS(1024, 4) PCONV_ROWS(1024, 8) PCONV_ROWS(1024, 16)
         if (!done) hipLaunchKernelGGL((distill_kernel<DT, 1024, 0>), dim3((unsigned)rows), dim3(1024), lds, st, a);
 #undef PCONV_ROWS
         PCONV_HIP(hipGetLastError());
