@@ -111,7 +111,8 @@ int pconv_activation_grad(const void* dy, long long lddy, const void* z, long lo
  *   gamma, beta  device, float[D], or NULL for ones / zeros
  *   mean, rstd   device, float[rows]: receive the statistics for the backward pass, or NULL (each of its own)
  *   rows 0.., D 1.., eps >= 0
- * The variance is taken around the mean (two passes over the row, the second from registers or cache).
+ * The variance is taken around the mean (two passes over the row, the second from registers or cache), and x - mean is good to
+ * units of the row's spread, however far from 0 the row lies: equal values give beta and 1 / sqrt(eps).
  * PCONV_EINVAL also for an eps that is negative or not a number.
  */
 int pconv_layer_norm(const void* x, long long ldx, const float* gamma, const float* beta, float eps, void* y, long long ldy,

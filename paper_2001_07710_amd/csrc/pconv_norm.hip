@@ -1,15 +1,17 @@
 // Layer norm over the rows of a matrix, forward and backward (pconv_dense.h).  Memory bounds both: x in and y out, and dy and x
 // in and dx out.
 //
-// A row is held in registers by TPR threads, Q pieces of 16 bytes each, so that it is read once: mean, then the squares around
-// it (or, backward, the two sums of g and g * h), each a reduction over those threads by shuffles, across waves through LDS.
+// A row is held in registers by TPR threads, Q pieces of 16 bytes each, so that it is read once: sum, then the sums of the deviations
+// from the mean and of their squares (or, backward, the two sums of g and g * h), each a reduction over those threads by shuffles, across
+// waves through LDS.  The sum's and the quotient's roundings leave the first mean off by units of the row's level, which may be more than
+// its spread; the deviations' own mean, `rest`, is what is missing to it (deviations of values near the mean are exact).
 // Workgroups walk over the rows, several short ones at a time, the next ones under way while these are worked on, so that a
 // thread's gamma and beta stay in registers too; in the backward pass so do its columns' sums of dy * h and dy, which meet at the
 // end: the threads with the same columns in LDS, the workgroups in the workspace, one part for a compute unit, added in a second launch.
 // Longer rows (than 1024 threads hold) are read twice or three times, from the caches.
-// 16384 x 4096, bf16: forward 45 us (5.9 TB/s, part of it from the cache behind L2), backward 78 us with the column sums (5.2 TB/s; a
-// copy reaches 5.17).  200704 x 64, fp16: forward 14 us (3.6 TB/s), backward 20 (3.9): there a wave's row is one load of its
-// lanes, and the shuffles of eight rows at a time are a third of its instructions.
+// 16384 x 4096, bf16: forward 48 us (5.5 TB/s, part of it from the cache behind L2), backward 77 us with the column sums (5.2 TB/s; a
+// copy reaches 5.17).  200704 x 64, fp16: forward 15 us (3.4 TB/s), backward 20 (3.9): there a wave's row is one load of its
+// lanes, and the shuffles of eight rows at a time are a third of its instructions.  (Forward without `rest`: 47 and 14.2.)
 #include <type_traits>
 
 #include "pconv_dense_util.h"
@@ -25,15 +27,31 @@ __device__ __forceinline__ float lanes_sum(float v) {
     return v;
 }
 
+// The sums of two values, at the price of one more exchange than those of one: even lanes take the first further, odd ones the second.
+template <int L>
+__device__ __forceinline__ void lanes_sums(float& a, float& b) {
+    const bool odd = threadIdx.x & 1;
+    float v = (odd ? b : a) + __shfl_xor(odd ? a : b, 1, 64);
+#pragma unroll
+    for (int d = 2; d < L; d *= 2) v += __shfl_xor(v, d, 64);
+    const float other = __shfl_xor(v, 1, 64);
+    a = odd ? other : v;
+    b = odd ? v : other;
+}
+
 // Sums of N values over the TPR threads that hold a row (of THREADS that meet at the barrier).  The waves' sums lie in one half of
-// `room` or the other by turns, so that one barrier is enough.
-template <int TPR, int N>
+// `room` or the other by turns, so that one barrier is enough.  PAIRS: two by two (not where registers are short: the backward pass of
+// 16384 x 4096 takes 90 us with it, 77 without).
+template <int TPR, int N, bool PAIRS = false>
 struct RowSum {
     float (*room)[N][16];
     int turn = 0;
     __device__ __forceinline__ void operator()(float (&v)[N]) {
+        constexpr int L = TPR < 64 ? TPR : 64;
 #pragma unroll
-        for (int n = 0; n < N; ++n) v[n] = lanes_sum<(TPR < 64 ? TPR : 64)>(v[n]);
+        for (int n = 0; n < N; n += PAIRS ? 2 : 1)
+            if constexpr (PAIRS) lanes_sums<L>(v[n], v[n + 1]);
+            else v[n] = lanes_sum<L>(v[n]);
         if constexpr (TPR > 64) {
             constexpr int W = TPR / 64;
             const int wave = threadIdx.x >> 6, first = wave / W * W;
@@ -72,6 +90,20 @@ __device__ __forceinline__ void load_columns(const float* v, int d, int D, float
     }
 }
 
+// v / D, rounded once, from v * (1 / D) and what that leaves (which is NaN where v is infinite)
+struct Mean {
+    float D, inv;
+    __device__ __forceinline__ float operator()(float v) const {
+        const float q = v * inv, left = fmaf(-q, D, v);
+        return left == left ? fmaf(left, inv, q) : q;
+    }
+};
+// 1 / sqrt(variance + eps) from the mean of the squares around a value that the mean is `rest` away from (NaN stays)
+__device__ __forceinline__ float rstd_of(float squares, float rest, float eps) {
+    const float variance = squares - rest * rest;
+    return 1.f / sqrtf((variance < 0.f ? 0.f : variance) + eps);
+}
+
 struct NormArgs {
     const void* x;
     const void* dy;
@@ -108,8 +140,9 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const NormArgs p) {
     typedef typename Store<DT>::T T;
     typedef typename Store<DT>::V V;
     constexpr int P = Store<DT>::kPer, GROUPS = THREADS / TPR;
-    __shared__ float room[2][U][16];
+    __shared__ float room[2][U][16], pair_room[2][2 * U][16];
     RowSum<TPR, U> row_sum{room};
+    RowSum<TPR, 2 * U, true> row_sums{pair_room};
     const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
     const long long step = (long long)gridDim.x * GROUPS, first = (long long)blockIdx.x * GROUPS + group;
     const long long turns = (p.rows + step * U - 1) / (step * U);    // (the same for every thread: row_sum has barriers)
@@ -121,13 +154,13 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const NormArgs p) {
         load_columns(p.gamma, (t + q * TPR) * P, p.D, 1.f, 1.f, gamma[q]);
         load_columns(p.beta, (t + q * TPR) * P, p.D, 0.f, 0.f, beta[q]);
     }
-    const float inv = 1.f / (float)p.D;
+    const Mean mean_of{(float)p.D, 1.f / (float)p.D};
     for (long long k = 0; k < turns; ++k) {
         const long long r0 = k * step * U + first;
         // (the next rows are under way while these are worked on)
         const Rows<DT, TPR, Q, U> now = rows;
         if (k + 1 < turns) rows.load(p.x, p.ldx, r0 + step * U, step, p.rows, p.D, t);
-        float mean[U], rstd[U];
+        float mean[U], s[2 * U], away[U][Q][P];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             mean[u] = 0.f;
@@ -141,36 +174,44 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const NormArgs p) {
         row_sum(mean);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            mean[u] *= inv;
-            rstd[u] = 0.f;
+            mean[u] *= mean_of.inv;
+            s[2 * u] = s[2 * u + 1] = 0.f;
 #pragma unroll
             for (int q = 0; q < Q; ++q) {
                 const V v = __builtin_bit_cast(V, now.raw[u][q]);
+                const int n = p.D - (t + q * TPR) * P;
+                // (what is behind the row is held as zeros, which deviate by nothing from a mean of 0)
+                const float m = n > 0 ? mean[u] : 0.f;
+#pragma unroll
+                for (int e = 0; e < P; ++e) away[u][q][e] = (float)v[e] - m;
+                if (n > 0 && n < P) {
+#pragma unroll
+                    for (int e = 1; e < P; ++e) away[u][q][e] = e < n ? away[u][q][e] : 0.f;
+                }
 #pragma unroll
                 for (int e = 0; e < P; ++e) {
-                    const float d = (float)v[e] - mean[u];
-                    rstd[u] += (t + q * TPR) * P + e < p.D ? d * d : 0.f;
+                    s[2 * u] += away[u][q][e];
+                    s[2 * u + 1] = fmaf(away[u][q][e], away[u][q][e], s[2 * u + 1]);
                 }
             }
         }
-        row_sum(rstd);
+        row_sums(s);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const long long r = r0 + u * step;
             if (r >= p.rows) break;
-            rstd[u] = 1.f / sqrtf(rstd[u] * inv + p.eps);
+            const float rest = mean_of(s[2 * u]), rstd = rstd_of(mean_of(s[2 * u + 1]), rest, p.eps);
             if (t == 0) {
-                if (p.mean) p.mean[r] = mean[u];
-                if (p.rstd) p.rstd[r] = rstd[u];
+                if (p.mean) p.mean[r] = mean[u] + rest;
+                if (p.rstd) p.rstd[r] = rstd;
             }
             T* const y = static_cast<T*>(p.out) + r * p.ldo;
 #pragma unroll
             for (int q = 0; q < Q; ++q) {
-                const V v = __builtin_bit_cast(V, now.raw[u][q]);
                 const int d = (t + q * TPR) * P, n = p.D - d;
                 V o;
 #pragma unroll
-                for (int e = 0; e < P; ++e) o[e] = (T)(((float)v[e] - mean[u]) * rstd[u] * gamma[q][e] + beta[q][e]);
+                for (int e = 0; e < P; ++e) o[e] = (T)fmaf((away[u][q][e] - rest) * rstd, gamma[q][e], beta[q][e]);
                 if (n >= P) store16(y + d, __builtin_bit_cast(uint4v, o));
                 else
 #pragma unroll
@@ -323,12 +364,13 @@ __device__ __forceinline__ void load_eight(const typename Store<DT>::T* p, int n
 template <int DT>
 __global__ __launch_bounds__(kLong) void norm_long_kernel(const NormArgs p) {
     typedef typename Store<DT>::T T;
-    __shared__ float room[2][1][16];
+    __shared__ float room[2][1][16], pair_room[2][2][16];
     RowSum<kLong, 1> row_sum{room};
+    RowSum<kLong, 2, true> row_sums{pair_room};
     for (long long r = blockIdx.x; r < p.rows; r += gridDim.x) {
         const T* const x = static_cast<const T*>(p.x) + r * p.ldx;
         T* const y = static_cast<T*>(p.out) + r * p.ldo;
-        float sum[1] = {}, squares[1] = {};
+        float sum[1] = {}, s[2] = {};
         along_row(p.D, [&](int d, auto whole) {
             float v[8];
             load_eight<DT, whole>(x + d, p.D - d, v);
@@ -341,12 +383,16 @@ __global__ __launch_bounds__(kLong) void norm_long_kernel(const NormArgs p) {
             float v[8];
             load_eight<DT, whole>(x + d, p.D - d, v);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) squares[0] += whole || d + e < p.D ? (v[e] - mean) * (v[e] - mean) : 0.f;
+            for (int e = 0; e < 8; ++e) {
+                const float away = whole || d + e < p.D ? v[e] - mean : 0.f;
+                s[0] += away;
+                s[1] = fmaf(away, away, s[1]);
+            }
         });
-        row_sum(squares);
-        const float rstd = 1.f / sqrtf(squares[0] / (float)p.D + p.eps);
+        row_sums(s);
+        const float rest = s[0] / (float)p.D, rstd = rstd_of(s[1] / (float)p.D, rest, p.eps);
         if (threadIdx.x == 0) {
-            if (p.mean) p.mean[r] = mean;
+            if (p.mean) p.mean[r] = mean + rest;
             if (p.rstd) p.rstd[r] = rstd;
         }
         along_row(p.D, [&](int d, auto whole) {
@@ -355,7 +401,7 @@ __global__ __launch_bounds__(kLong) void norm_long_kernel(const NormArgs p) {
             load_columns(p.gamma, d, p.D, 1.f, 1.f, gamma);
             load_columns(p.beta, d, p.D, 0.f, 0.f, beta);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = (v[e] - mean) * rstd * gamma[e] + beta[e];
+            for (int e = 0; e < 8; ++e) v[e] = fmaf((v[e] - mean - rest) * rstd, gamma[e], beta[e]);
             store8<DT>(y + d, whole ? 8 : p.D - d, v);
         });
     }

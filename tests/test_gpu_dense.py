@@ -437,6 +437,55 @@ def test_layer_norm_without_weights_in_place_and_of_equal_values(dt):
     assert z[rest].tobytes() == y[rest].tobytes() and np.isnan(z[4]).all() and np.isnan(z[3, 5])
 
 
+@pytest.mark.parametrize("dt", TYPES)
+def test_layer_norm_of_rows_of_equal_values_is_exact(dt):
+    """Rows of one value, at every spread of a row over threads.  The first mean is off by k units of the value's last place: a sum of 16-bit
+    values is exact but for its last additions (k <= 10), one of fp32 values passes 36 additions, then comes a product with 1 / D (k <= 38).  All deviations are
+    then that k, exactly, and their sum and their squares' are whole multiples below 2^24 units (38^2 * 8,200 = 1.2e7): the mean is the value,
+    the variance 0 and y beta.  rstd: a root, a quotient and eps, two units each."""
+    rng = np.random.default_rng(24)
+    levels = rounded(np.array([0.1, 100, 1000, 4000, 30000, -777, 1 / 3, -61000.0]), dt)
+    for Dn in (26, 41, 100, 200, 500, 1000, 1025, 2000, 4001, 8191, 8200, 16383, 16400):
+        if dt == "f32" and Dn > 8200:
+            continue
+        rows = 5 * len(levels) if Dn < 600 else len(levels)
+        x = levels[np.arange(rows) % len(levels)][:, None].repeat(Dn, 1)
+        gamma, beta = (rng.standard_normal(Dn).astype(np.float32) for _ in range(2))
+        say("equal values", dt, rows, Dn)
+        for eps in (1e-5, 0.0) if Dn <= 1025 else (1e-5,):
+            mx, my, mean, rstd = Mat(x, dt), empty(rows, Dn, dt), empty(1, rows, "f32"), empty(1, rows, "f32")
+            pc.layer_norm(mx, my, CODE[dt], rows, Dn, gamma=vec(gamma), beta=vec(beta), eps=eps, mean=mean, rstd=rstd, stream=stream())
+            assert np.array_equal(mean.get()[0], x[:, 0]), (dt, Dn, eps)
+            if eps:
+                assert np.array_equal(my.get(), rounded(beta, dt)[None, :].repeat(rows, 0)), (dt, Dn)
+                want = 1 / np.sqrt(float(np.float32(eps)))
+                assert (np.abs(rstd.get()[0] - want) <= 6 * U32 * want).all(), (dt, Dn)
+            else:                                                      # 0 / 0, like the formula
+                assert np.isnan(my.get()).all() and np.isinf(rstd.get()[0]).all(), (dt, Dn)
+
+
+@pytest.mark.parametrize("dt", TYPES)
+def test_layer_norm_of_rows_far_from_zero(dt):
+    """Rows whose spread is small against their level: x - mean is exact around the first mean, so that everything behind it is relative to
+    the spread, sums of 64 units as in the test above of rows near zero; the first mean, 40 units of the level off at most, is less than half
+    of the spread away, whose square is a quarter of the variance that is taken off again: 128 units for the mean, 192 |h| for rstd."""
+    rng = np.random.default_rng(25)
+    step = {"f32": 2.0 ** -6, "f16": 0.5, "bf16": 4.0}[dt]
+    for Dn in (41, 100, 300, 1000, 2000, 4001, 8191, 16383, 40000):
+        rows = 30 if Dn < 600 else 6
+        x = 1000.0 + step * (rng.integers(-2, 3, (rows, Dn)) if dt == "f32" else rng.random((rows, Dn)) < 0.1)
+        gamma = rng.standard_normal(Dn).astype(np.float32)
+        say("far from zero", dt, rows, Dn)
+        assert np.array_equal(rounded(x, dt), x)
+        mx, my, mean, rstd = Mat(x, dt), empty(rows, Dn, dt), empty(1, rows, "f32"), empty(1, rows, "f32")
+        pc.layer_norm(mx, my, CODE[dt], rows, Dn, gamma=vec(gamma), mean=mean, rstd=rstd, stream=stream())
+        y, m, s = D.layer_norm(x, gamma, None, float(np.float32(1e-5)))
+        h = (x - m[:, None]) * s[:, None]
+        assert (np.abs(mean.get()[0] - m) <= U32 * np.abs(m) + 64 * U32 / s).all(), (dt, Dn)
+        assert (np.abs(rstd.get()[0] - s) <= 96 * U32 * s).all(), (dt, Dn)
+        _close(my.get(), y, dt, (128 + 192 * np.abs(h)) * U32 * np.abs(gamma) + 4 * U32 * np.abs(y))
+
+
 # -------------------------------------------------------------------------------------------------------------- distillation
 
 def _distill(s, idx, val, dt, T, weight=None, pad=0, ahead=0, gpad=None, gahead=None, what=("loss", "grad", "stats")):
