@@ -152,7 +152,7 @@ int pconv_layer_norm_grad(const void* dy, long long lddy, const void* x, long lo
  *   grad     device, dtype[R][V], row stride ldg, or NULL; may be logits itself with ldg = ldl
  *   stats    device, float[R][2], or NULL: receives what pconv_distill_grad needs of the row's softmax (the largest logit
  *            and the sum of exp((s - largest) / T)); zeros for a row that is left out
- *   R 0.., V 1.., k 1..1024, T > 0 and finite
+ *   R 0.., V 1.., k 1..1024, T > 0 and finite, log2(e) / T too (T from 4.25e-39 on; PCONV_EINVAL otherwise)
  * A row without entries, whose entries are all -inf, or of weight 0 is left out: loss and gradient 0, whatever its logits hold
  * (padding).  In other rows a logit of -inf has q = 0 (loss +inf if the teacher gives it more), +inf or NaN makes NaN.
  * loss, grad and stats are three results of one call; at least one is asked for (PCONV_EINVAL).

@@ -338,7 +338,8 @@ int distill(const void* logits, long long ldl, const int32_t* indices, const flo
     if (!is_dtype(dtype)) return PCONV_EINVAL;
     if (R < 0 || V < 1 || k < 1) return PCONV_ESHAPE;
     if (k > kMostEntries) return PCONV_EUNSUPPORTED;
-    if (!(temperature > 0.f) || !(temperature < __builtin_inff()) || !(1.f / temperature < __builtin_inff())) return PCONV_EINVAL;
+    const double c = 1.4426950408889634 / (double)temperature;
+    if (!(temperature > 0.f) || !(temperature < __builtin_inff()) || !(c < 0x1.ffffffp127)) return PCONV_EINVAL;    // (c: finite in fp32)
     for (int rc : {check_stride(&ldl, V), grad ? check_stride(&ldg, V) : PCONV_OK})
         if (rc) return rc;
     if (!asked) return PCONV_EINVAL;
@@ -355,7 +356,6 @@ int distill(const void* logits, long long ldl, const int32_t* indices, const flo
     a.given = given; a.stats = stats;
     a.V = V; a.k = k;
     a.t = temperature; a.inv_t = 1.f / temperature;
-    const double c = 1.4426950408889634 / (double)temperature;
     a.c = (float)c; a.c_low = (float)(c - (double)a.c);
     hipStream_t st = static_cast<hipStream_t>(stream);
     return dtype == PCONV_F32   ? launch_distill<PCONV_F32>(a, R, st)

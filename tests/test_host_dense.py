@@ -128,6 +128,15 @@ def test_distillation_refuses(dtype):
     assert c(X, W, Z, B, Y, dtype, 4, 100, 3, 0.0) == pc.EINVAL
 
 
+def test_distillation_refuses_temperatures_whose_exponents_overflow():
+    """The kernel takes exp(d / T) as 2^(d * log2(e) / T): log2(e) / T is finite from 1.4427 / (2^128 - 2^103) = 4.2397e-39 on."""
+    for T in (1e-45, 2.9e-39, 2.95e-39, 3e-39, 4.2e-39):
+        assert code(pc.distill, X, W, Z, pc.F16, 4, 100, 3, T, loss=B, grad=Y) == pc.EINVAL
+        assert code(pc.distill_grad, X, W, Z, B, Y, pc.F16, 4, 100, 3, T) == pc.EINVAL
+    for T in (4.25e-39, 1e-38, 1e-30, 1e30, 3.4e38):
+        pc.distill(None, None, None, pc.F16, 0, 100, 3, T, loss=B)
+
+
 def test_sizes_at_the_end_of_their_range():
     """Plans of the largest sizes: no overflow, a workspace of whole parts, and none where there is nothing to share."""
     pc.ensure_built()
