@@ -30,7 +30,7 @@ struct DistillArgs {
     float* stats;
     long long ldl, ldg;
     int V, k;
-    float inv_t, t;
+    float t;
     float c, c_low;            // log2(e) / T, and what is missing to it
 };
 
@@ -266,18 +266,19 @@ __global__ __launch_bounds__(THREADS, waves_per_simd(THREADS, Q)) void distill_k
             }
         }
     }
-    // the loss, and p in the place of t
+    // the loss, and p in the place of t.  T * (log p - log q) = (t - largest t) - (s - largest s) - T * (log total - log norm): no quotient
+    // by T, and no T^2, which overflow where the loss does not
     if (t < 64) {
-        const float log_total = logf(total), log_norm = logf(norm);
+        const float between = p.t * (logf(total) - logf(norm));
         float loss = 0.f;
         for (int j = lane; j < p.k; j += 64) {
             if (index[j] < 0) continue;
-            const float d = prob[j] - top, log_p = d * p.inv_t - log_total, mine = exp_over_t<true>(d, c, c_low) / total;
-            if (!(mine == 0.f)) loss += mine * (log_p - ((own[j] - largest) * p.inv_t - log_norm));
+            const float d = prob[j] - top, mine = exp_over_t<true>(d, c, c_low) / total;
+            if (!(mine == 0.f)) loss += mine * (d - (own[j] - largest) - between);
             prob[j] = mine;
         }
         loss = wave_reduce(loss, plus);
-        if (p.loss && t == 0) p.loss[r] = w * p.t * p.t * loss;
+        if (p.loss && t == 0) p.loss[r] = scale * loss;
     }
     if (!p.grad) return;
     __syncthreads();
@@ -355,7 +356,7 @@ int distill(const void* logits, long long ldl, const int32_t* indices, const flo
     a.grad = grad; a.ldg = ldg;
     a.given = given; a.stats = stats;
     a.V = V; a.k = k;
-    a.t = temperature; a.inv_t = 1.f / temperature;
+    a.t = temperature;
     a.c = (float)c; a.c_low = (float)(c - (double)a.c);
     hipStream_t st = static_cast<hipStream_t>(stream);
     return dtype == PCONV_F32   ? launch_distill<PCONV_F32>(a, R, st)

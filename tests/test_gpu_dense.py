@@ -647,6 +647,34 @@ def test_distillation_takes_the_teachers_logits_by_their_differences():
     assert loss.tobytes() == same_loss.tobytes() and grad.tobytes() == same_grad.tobytes()
 
 
+def test_distillation_at_temperatures_whose_square_or_quotients_pass_32_bits():
+    """Logits of whole 2^-10, whose differences are exact.  Cold: one entry has everything (p = q = 1 at their largest), so that the loss is T
+    times what the network's logit there is short of its largest, one product, and the gradient -T and T.  Hot: all exponentials are 1, so
+    that the loss is T^2 * log(V / k), the difference of two logarithms of two units of at most 2 log(V), and two products."""
+    rng = np.random.default_rng(35)
+    R, V, k = 5, 200, 7
+    s = rng.permuted(np.arange(V) / 1024.0 * np.ones((R, 1)), axis=1)
+    idx = np.stack([rng.permutation(V)[:k] for _ in range(R)]).astype(np.int32)
+    val = rng.permuted(np.arange(k) / 4.0 * np.ones((R, 1)), axis=1)
+    best = np.take_along_axis(idx, val.argmax(1)[:, None], 1)[:, 0]
+    short = s.max(1) - s[np.arange(R), best]
+    for T in (1e-20, 1e-25, 1e-30):
+        T32 = float(np.float32(T))
+        loss, grad = _distill(s, idx, val, "f32", T)[:2]
+        assert (np.abs(loss - T32 * short) <= 2 * U32 * T32 * short).all(), T
+        want = np.zeros((R, V))
+        want[np.arange(R), s.argmax(1)] += T32
+        want[np.arange(R), best] -= T32
+        assert (np.abs(grad - want) <= 8 * U32 * T32).all(), T
+    for T, V2, k2 in ((2e19, 4, 2), (1e19, 300, 40), (1.8e19, 3, 3), (1e25, 1, 1), (3e38, 1, 1), (1e19, 2, 2)):
+        T32 = float(np.float32(T))
+        loss, grad = _distill(s[:, :V2], np.arange(k2)[None, :].repeat(R, 0), val[:, :1].repeat(k2, 1), "f32", T)[:2] if V2 <= V else \
+            _distill(np.zeros((R, V2)), np.arange(k2)[None, :].repeat(R, 0), np.zeros((R, k2)), "f32", T)[:2]
+        want = T32 * T32 * np.log(V2 / k2)
+        assert (np.abs(loss - want) <= T32 * T32 * 8 * U32 * 2 * np.log(V2)).all(), (T, V2, k2, loss, want)
+        assert np.isfinite(grad).all()
+
+
 def test_small_probabilities_are_as_exact_as_large_ones_in_32_bits():
     """Logits of whole 2^-10, whose differences are exact, down to 60 T below the largest.  In units of 2^-24: the sum of 400 exponentials
     in 14 additions on top of each other 14, its exponentials 4, the element's exponential 4, two products and two quotients 4: 26, with
