@@ -128,20 +128,48 @@ constexpr float kSqrtHalf = 0.70710678118654752f, kSqrt2OverPi = 0.7978845608028
 // is; `bounded`, one instruction, does not: for curves, which z itself multiplies.
 __device__ __forceinline__ float tamed(float z) { return z > 100.f ? 100.f : z < -100.f ? -100.f : z; }
 __device__ __forceinline__ float bounded(float z) { return __builtin_amdgcn_fmed3f(z, -100.f, 100.f); }
+constexpr float kLog2E = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
+// An exponent in two parts, `low` being what the first one's rounding left.  WIDE (fp32): rounded as one number an exponent x costs 2^x some
+// |x| units, up to a hundred in the tails; with the rest put right behind the exponential that is one.  Otherwise `low` is 0: a hundred
+// units are nothing that 16 bits keep.
+struct Exponent {
+    float x, low;
+};
+template <bool WIDE>
+__device__ __forceinline__ float exp2_of(const Exponent& a) {
+    const float e = __builtin_amdgcn_exp2f(a.x);
+    if constexpr (!WIDE) return e;
+    return a.x > 127.f ? e : fmaf(e, a.low * kLn2, e);             // (2^x may be infinite)
+}
+// t * (c + c_low)
+template <bool WIDE>
+__device__ __forceinline__ Exponent exponent(float t, float c, float c_low) {
+    Exponent a{t * c, 0.f};
+    if constexpr (WIDE) a.low = fmaf(t, c_low, fmaf(t, c, -a.x));
+    return a;
+}
 // 1 / (1 + 2^x).  (v_exp_f32 and v_rcp_f32 are good to one unit of 32 bits each; an IEEE division is ten instructions.)
-__device__ __forceinline__ float falling(float x) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x)); }
-constexpr float kLog2E = 1.44269504088896341f;
+template <bool WIDE>
+__device__ __forceinline__ float falling(const Exponent& a) { return __builtin_amdgcn_rcpf(1.f + exp2_of<WIDE>(a)); }
 
 __device__ __forceinline__ float relu(float z) { return z < 0.f ? 0.f : z; }                    // (NaN stays)
 __device__ __forceinline__ float relu_slope(float z) { return z > 0.f ? 1.f : z == z ? 0.f : z; }
-// Phi(t), the normal distribution, and e = exp(-t^2 / 2).  WIDE: from erfc, which has no cancellation in the tail either.  Otherwise the
-// tail as e times a polynomial in k = 1 / (1 + 0.27 |t|), fitted to exp(t^2 / 2) * Phi(-t) over 0 .. 13.2 for the least relative error:
-// 1.2e-6, with the roundings 5e-6 at most, of the tail, a hundredth of fp16's half step.  (8192 x 4096 x 4096, bf16: 198 us without an
-// activation, 248 with erff, 212 with the polynomial.  fp32 products wait for the matrix cores in any case.)
+// Phi(t), the normal distribution, and e = exp(-t^2 / 2).  WIDE: from erfc, which has no cancellation in the tail either, with the rounding
+// of its argument put right by its slope.  Otherwise the tail as e times a polynomial in k = 1 / (1 + 0.27 |t|), fitted to
+// exp(t^2 / 2) * Phi(-t) over 0 .. 13.2 for the least relative error: 1.2e-6, with the roundings 5e-6 at most, of the tail, a hundredth of
+// fp16's half step.  (8192 x 4096 x 4096, bf16: 198 us without an activation, 248 with erff, 212 with the polynomial.  fp32 products wait
+// for the matrix cores in any case.)
 template <bool WIDE>
 __device__ __forceinline__ float normal_share(float t, float& e) {
+    if constexpr (WIDE) {
+        const float h = t * t, x = -kSqrtHalf * t;
+        Exponent a = exponent<true>(h, -0.5f * kLog2E, -9.62981517e-9f);
+        a.low = fmaf(fmaf(t, t, -h), -0.5f * kLog2E, a.low);
+        e = exp2_of<true>(a);
+        const float left = fmaf(-1.21016175e-8f, t, fmaf(-kSqrtHalf, t, -x));
+        return fmaf(-0.56418958f * left, e, 0.5f * erfcf(x));      // (erfc'(x) / 2 = -exp(-x^2) / sqrt(pi))
+    }
     e = __builtin_amdgcn_exp2f(-0.5f * kLog2E * t * t);
-    if constexpr (WIDE) return 0.5f * erfcf(-kSqrtHalf * t);
     const float k = __builtin_amdgcn_rcpf(fmaf(0.27f, fabsf(t), 1.f));
     const float poly = k * fmaf(k, fmaf(k, fmaf(k, fmaf(k, fmaf(k, fmaf(k, -0.060592773f, 0.157589721f), -0.0228579642f), 0.116564072f),
                                                 0.0932392658f), 0.108363624f), 0.107693477f);
@@ -159,19 +187,32 @@ __device__ __forceinline__ float gelu_slope(float z) {
     const float t = tamed(z), share = normal_share<WIDE>(t, e);
     return fmaf(t * kInvSqrt2Pi, e, share);
 }
-// (1 + tanh(u)) / 2 = 1 / (1 + exp(-2u)): no cancellation where the curve nears 0
+// (1 + tanh(u)) / 2 = 1 / (1 + exp(-2u)): no cancellation where the curve nears 0.  -2u * log2(e) = t * (k + m t^2)
+template <bool WIDE>
 __device__ __forceinline__ float gelu_tanh_share(float t) {
     constexpr float k = -2.f * kSqrt2OverPi * kLog2E;
-    return falling(t * fmaf(k * 0.044715f, t * t, k));
+    if constexpr (WIDE) {
+        constexpr float k0 = -2.30220819f, k0_low = -1.29484024e-8f, m = -0.102943242f, m_low = 2.01619854e-9f;
+        const float h = t * t, p = m * h, p_low = fmaf(m, h, -p) + fmaf(m, fmaf(t, t, -h), m_low * h);
+        const float c = k0 + p, b = c - k0, c_low = (k0 - (c - b)) + (p - b) + (p_low + k0_low);     // (the sum's rounding, either larger)
+        return falling<true>(exponent<true>(t, c, c_low));
+    }
+    return falling<false>({t * fmaf(k * 0.044715f, t * t, k), 0.f});
 }
-__device__ __forceinline__ float gelu_tanh(float z) { return z * gelu_tanh_share(bounded(z)); }
+template <bool WIDE>
+__device__ __forceinline__ float gelu_tanh(float z) { return z * gelu_tanh_share<WIDE>(bounded(z)); }
+template <bool WIDE>
 __device__ __forceinline__ float gelu_tanh_slope(float z) {
-    const float t = tamed(z), s = gelu_tanh_share(t);
+    const float t = tamed(z), s = gelu_tanh_share<WIDE>(t);
     return fmaf(t * s * (1.f - s), fmaf(6.f * kSqrt2OverPi * 0.044715f, t * t, 2.f * kSqrt2OverPi), s);
 }
-__device__ __forceinline__ float silu(float z) { return z * falling(-kLog2E * bounded(z)); }
+template <bool WIDE>
+__device__ __forceinline__ float silu_share(float t) { return falling<WIDE>(exponent<WIDE>(t, -kLog2E, -1.92596303e-8f)); }
+template <bool WIDE>
+__device__ __forceinline__ float silu(float z) { return z * silu_share<WIDE>(bounded(z)); }
+template <bool WIDE>
 __device__ __forceinline__ float silu_slope(float z) {
-    const float t = tamed(z), s = falling(-kLog2E * t);
+    const float t = tamed(z), s = silu_share<WIDE>(t);
     return s * fmaf(t, 1.f - s, 1.f);
 }
 
@@ -185,8 +226,8 @@ __device__ __forceinline__ void activate8(float v[R][8], int act) {
     switch (act) {
         case PCONV_ACT_RELU: PCONV_EACH(relu);
         case PCONV_ACT_GELU: PCONV_EACH(gelu<DT == PCONV_F32>);
-        case PCONV_ACT_GELU_TANH: PCONV_EACH(gelu_tanh);
-        case PCONV_ACT_SILU: PCONV_EACH(silu);
+        case PCONV_ACT_GELU_TANH: PCONV_EACH(gelu_tanh<DT == PCONV_F32>);
+        case PCONV_ACT_SILU: PCONV_EACH(silu<DT == PCONV_F32>);
         default: break;
     }
 #undef PCONV_EACH
@@ -200,8 +241,8 @@ __device__ __forceinline__ void times_slope8(float v[R][8], const float z[R][8],
     switch (act) {
         case PCONV_ACT_RELU: PCONV_EACH(relu_slope);
         case PCONV_ACT_GELU: PCONV_EACH(gelu_slope<DT == PCONV_F32>);
-        case PCONV_ACT_GELU_TANH: PCONV_EACH(gelu_tanh_slope);
-        case PCONV_ACT_SILU: PCONV_EACH(silu_slope);
+        case PCONV_ACT_GELU_TANH: PCONV_EACH(gelu_tanh_slope<DT == PCONV_F32>);
+        case PCONV_ACT_SILU: PCONV_EACH(silu_slope<DT == PCONV_F32>);
         default: break;
     }
 #undef PCONV_EACH

@@ -225,6 +225,39 @@ def test_the_tail_of_gelu(dt):
     _close(y, want, dt, (v * v + 64) * U32 * np.abs(want))
 
 
+def _tail(act, v):
+    """(curve, slope, what the slope's rounding errors are relative to) at v <= 0, without cancellation; v as far as fp32 has the curve."""
+    from math import erfc, sqrt
+    if act == "gelu":
+        s = np.vectorize(lambda t: erfc(-t / sqrt(2)) / 2)(v)
+        rise = v * np.exp(-v * v / 2) / np.sqrt(2 * np.pi)
+    else:
+        c = 2 * np.sqrt(2 / np.pi)
+        u, du = (v, 1.0) if act == "silu" else (c * (v + 0.044715 * v ** 3), c * (1 + 3 * 0.044715 * v * v))
+        s = 1 / (1 + np.exp(-u))
+        rise = v * s / (1 + np.exp(u)) * du
+    return v * s, s + rise, s + np.abs(rise)
+
+
+@pytest.mark.parametrize("act", ["gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("dt", TYPES)
+def test_the_tails_of_activations_and_of_their_slopes(dt, act):
+    """Relative to the tail itself, in units of 2^-24.  fp32: the exponential 2, its argument's remainder 1, 1 + e 1, the reciprocal 2, z times
+    it 1 (GELU: erfc 16, half of the slope's product 2): 8 and 20; the slope's factors and sum 8 more.  16 bits: the exponent x rounded up to
+    three times costs 3 |x| units, the polynomial of GELU's tail 20, the other roundings 16."""
+    far = {"gelu": 12.5, "gelu_tanh": 9.5, "silu": 80.0}[act]
+    v = rounded(-np.linspace(0, far, 4001), dt)[:, None]
+    y, z = _linear(v, np.ones((1, 1)), dt, None, None, act, False, 0, 0)
+    assert np.array_equal(z, v)
+    curve, slope, size = _tail(act, v)
+    x = np.abs({"gelu": v * v / 2, "gelu_tanh": 1.6 * (v + 0.044715 * v ** 3), "silu": v}[act])
+    units = (20 if act == "gelu" else 8) if dt == "f32" else 3 * x + 36
+    _close(y, curve, dt, units * U32 * np.abs(curve))
+    one, mv, mo = Mat(np.ones(v.shape), dt), Mat(v, dt), empty(*v.shape, dt)
+    pc.activation_grad(one, mv, mo, CODE[dt], *v.shape, ACT[act], stream=stream())
+    _close(mo.get(), slope, dt, (units + 8) * U32 * size)
+
+
 @pytest.mark.parametrize("act", D.ACTS)
 @pytest.mark.parametrize("dt", TYPES)
 def test_activations_and_their_slopes(dt, act):
