@@ -156,9 +156,9 @@ __device__ __forceinline__ float relu(float z) { return z < 0.f ? 0.f : z; }    
 __device__ __forceinline__ float relu_slope(float z) { return z > 0.f ? 1.f : z == z ? 0.f : z; }
 // Phi(t), the normal distribution, and e = exp(-t^2 / 2).  WIDE: from erfc, which has no cancellation in the tail either, with the rounding
 // of its argument put right by its slope.  Otherwise the tail as e times a polynomial in k = 1 / (1 + 0.27 |t|), fitted to
-// exp(t^2 / 2) * Phi(-t) over 0 .. 13.2 for the least relative error: 1.2e-6, with the roundings 5e-6 at most, of the tail, a hundredth of
-// fp16's half step.  (8192 x 4096 x 4096, bf16: 198 us without an activation, 248 with erff, 212 with the polynomial.  fp32 products wait
-// for the matrix cores in any case.)
+// exp(t^2 / 2) * Phi(-t) over 0 .. 13.2 for the least relative error, 1.2e-6.  The roundings of t^2 and of the exponent add some t^2 units
+// of 2^-24: 1e-5 of the tail at t = 13, a fiftieth of fp16's half step.  (8192 x 4096 x 4096, bf16: 198 us without an activation, 248 with
+// erff, 212 with the polynomial.  fp32 products wait for the matrix cores in any case.)
 template <bool WIDE>
 __device__ __forceinline__ float normal_share(float t, float& e) {
     if constexpr (WIDE) {
