@@ -340,6 +340,125 @@ def test_a_row_does_not_depend_on_its_place_nor_on_its_neighbours(dt):
         assert np.array_equal(z[clean], y[clean]) and not np.isfinite(z[:, N - 2]).any() and not np.isfinite(z[3]).any()
 
 
+# M, N, K: the smallest tile, whole and ragged; the same split; few rows, split; the middle tile; the largest, two for some workgroups
+ALIKE = [(150, 140, 203), (192, 128, 256), (100, 130, 5000), (9, 70, 3000), (2100, 2200, 136), (4600, 6143, 200)]
+
+
+@pytest.mark.parametrize("act", D.ACTS)
+@pytest.mark.parametrize("dt", TYPES)
+def test_equal_rows_give_equal_results_in_every_epilogue(dt, act):
+    """Rows of whole and of ragged tiles leave by different ways, and rows of a window by different lanes: all the same, to the bit."""
+    import torch
+    rng = np.random.default_rng(16)
+    for M, N, K in ALIKE if act in ("none", "gelu") else ALIKE[:-1]:
+        alike = lambda n: torch.from_numpy(rounded(rng.standard_normal((1, n)), dt)).cuda().to(ttype(dt)).repeat(M, 1)  # noqa: E731
+        x, r, add, w = alike(K), alike(N), alike(K), vec(rng.standard_normal((N, K)) / np.sqrt(K)).to(ttype(dt))
+        bias = vec(rng.standard_normal(N))
+        say("alike", dt, act, M, N, K)
+        ws = Scratch(max(pc.linear_workspace(CODE[dt], M, N, K), pc.linear_grad_input_workspace(CODE[dt], M, N, K)))
+        for residual, flags, keep in ((None, 0, False), (r, 0, True), (r, pc.FLAG_RESIDUAL_FIRST, True), (r, pc.FLAG_RESIDUAL_FIRST, False)):
+            y, z = torch.full((M, N), 55.0, dtype=ttype(dt), device="cuda"), torch.full((M, N), 55.0, dtype=ttype(dt), device="cuda")
+            pc.linear(x, w, y, CODE[dt], M, N, K, bias=bias, residual=residual, z=z if keep else None, act=ACT[act], flags=flags,
+                      stream=stream(), **ws.args())
+            assert bool((y == y[0]).all()) and bool((z == z[0]).all()), (dt, act, M, N, K, flags, keep)
+        for more in (None, add):
+            dx = torch.full((M, K), 55.0, dtype=ttype(dt), device="cuda")
+            pc.linear_grad_input(r, w, dx, CODE[dt], M, N, K, z=x if act != "none" else None, act=ACT[act], add=more, stream=stream(),
+                                 **ws.args())
+            assert bool((dx == dx[0]).all()), (dt, act, M, N, K)
+        ws.check()
+
+
+@pytest.mark.parametrize("dt", TYPES)
+def test_arguments_of_activations_are_kept_exactly(dt):
+    """z of whole sixteenths, 9 + 4 at most: 208 of them, which eight bits hold."""
+    rng = np.random.default_rng(17)
+    x, w, r = whole(rng, (40, 16), 3) / 4, whole(rng, (72, 16), 3) / 4, whole(rng, (40, 72), 64) / 16
+    for act in D.ACTS:
+        for first in (False, True):
+            _, z = _linear(x, w, dt, None, r, act, first, 0, 0)
+            assert np.array_equal(z, D.linear(x, w, None, r, act, first)[1]), (dt, act, first)
+
+
+# (elements between rows, elements in front) of every matrix, each its own: all rows aligned; the first, the second operand alone not; neither
+APART = [[(8, 0), (16, 8), (24, 16), (32, 0), (40, 8)], [(3, 1), (16, 8), (5, 0), (0, 0), (9, 2)], [(8, 16), (7, 0), (2, 5), (11, 3), (0, 8)],
+         [(1, 3), (5, 1), (0, 2), (13, 0), (6, 7)]]
+
+
+@pytest.mark.parametrize("places", APART, ids=["aligned", "first", "second", "neither"])
+@pytest.mark.parametrize("dt", TYPES)
+def test_every_matrix_has_a_stride_of_its_own(dt, places):
+    """Square products, so that a stride taken for another's stays inside the matrices' buffers or reads marks; whole numbers, to the bit."""
+    import torch
+    rng = np.random.default_rng(18)
+    for n in (24, 200, 264):
+        say("apart", dt, n)
+        a, b, c, d = (whole(rng, (n, n), 3) for _ in range(4))
+        bias = whole(rng, n, 20)
+        ma, mb, mc, md, mo = ([Mat(v, dt, *at) for v, at in zip((a, b, c, d), places)] + [empty(n, n, dt, *places[4])])
+        mz = empty(n, n, dt, places[4][0], 3)
+        ws = Scratch(max(f(CODE[dt], n, n, n) for f in (pc.linear_workspace, pc.linear_grad_input_workspace, pc.linear_grad_weight_workspace)))
+        pc.linear(ma, mb, mo, CODE[dt], n, n, n, bias=vec(bias), residual=mc, z=mz, act=pc.ACT_RELU, ldx=ma.ld, ldw=mb.ld, ldr=mc.ld,
+                  ldy=mo.ld, stream=stream(), **ws.args())
+        y, z = D.linear(a, b, bias, c, "relu", False)
+        assert np.array_equal(mo.get(), rounded(y, dt)) and np.array_equal(mz.get(), rounded(z, dt))
+        pc.linear_grad_input(ma, mb, mo, CODE[dt], n, n, n, z=mc, act=pc.ACT_RELU, add=md, lddz=ma.ld, ldw=mb.ld, ldz=mc.ld, lda=md.ld,
+                             lddx=mo.ld, stream=stream(), **ws.args())
+        assert np.array_equal(mo.get(), rounded(D.linear_grad_input(a, b, c, "relu", d), dt))
+        dw, db = empty(n, n, "f32"), empty(1, n, "f32")
+        pc.linear_grad_weight(ma, mb, dw, CODE[dt], n, n, n, db=db, lddz=ma.ld, ldx=mb.ld, stream=stream(), **ws.args())
+        want = D.linear_grad_weight(a, b)
+        assert np.array_equal(dw.get(), want[0]) and np.array_equal(db.get()[0], want[1])
+        pc.activation_grad(ma, mb, mo, CODE[dt], n, n, pc.ACT_RELU, lddy=ma.ld, ldz=mb.ld, lddz=mo.ld, stream=stream())
+        assert np.array_equal(mo.get(), a * (b > 0))
+        ws.check()
+        # layer norm at strides of their own is layer norm at one: the same rows tightly packed, to the bit
+        ta, tb, to = Mat(a, dt), Mat(b, dt), empty(n, n, dt)
+        stats = [[torch.empty(n, device="cuda") for _ in range(2)] for _ in range(2)]
+        out = [[empty(1, n, "f32") for _ in range(2)] for _ in range(2)]
+        need = pc.layer_norm_grad_workspace(CODE[dt], n, n)
+        for (mx, mdy, my), (mean, rstd), (dg, dbeta) in zip(((ma, mb, mo), (ta, tb, to)), stats, out):
+            pc.layer_norm(mx, my, CODE[dt], n, n, gamma=vec(bias), beta=vec(bias), mean=mean, rstd=rstd, ldx=mx.ld, ldy=my.ld, stream=stream())
+            first = my.get()
+            ws = Scratch(need)
+            pc.layer_norm_grad(mdy, mx, my, mean, rstd, CODE[dt], n, n, gamma=vec(bias), dgamma=dg, dbeta=dbeta, lddy=mdy.ld, ldx=mx.ld,
+                               lddx=my.ld, stream=stream(), **ws.args())
+            second = my.get()
+            if mx is ma:
+                y, dx = first, second
+        assert y.tobytes() == first.tobytes() and dx.tobytes() == second.tobytes()
+        for one, other in zip(out[0] + [empty(1, 1, "f32")], out[1] + [empty(1, 1, "f32")]):
+            assert one.get().tobytes() == other.get().tobytes()
+        assert all(torch.equal(p, q) for p, q in zip(*stats))
+
+
+@pytest.mark.parametrize("dt", TYPES)
+def test_products_of_rows_that_lie_2_to_the_20_elements_apart(dt):
+    """The longest stride there is, in every matrix, at the smallest and (16 bits) the largest tile: offsets inside a tile pass 2^28 bytes."""
+    import torch
+    rng = np.random.default_rng(19)
+    ld = 1 << 20
+    for M, N, K in [(70, 90, 200), (5, 40, 333)] + ([(4096, 4096, 72)] if dt == "f16" else []):
+        say("far rows", dt, M, N, K)
+        x, w, r = whole(rng, (M, K), 3), whole(rng, (N, K), 2), whole(rng, (M, N), 30)
+
+        def far(a):
+            t = torch.empty((a.shape[0], ld), dtype=ttype(dt), device="cuda")[:, :a.shape[1]]
+            t.copy_(torch.from_numpy(a).cuda())
+            return t
+        fx, fw, fr, fy = far(x), far(w), far(r), far(np.full((M, N), 55.0))
+        ws = Scratch(max(f(CODE[dt], M, N, K) for f in (pc.linear_workspace, pc.linear_grad_input_workspace, pc.linear_grad_weight_workspace)))
+        pc.linear(fx, fw, fy, CODE[dt], M, N, K, residual=fr, ldx=ld, ldw=ld, ldr=ld, ldy=ld, stream=stream(), **ws.args())
+        assert np.array_equal(fy.double().cpu().numpy(), rounded(x @ w.T + r, dt))
+        pc.linear_grad_input(fr, fw, fx, CODE[dt], M, N, K, lddz=ld, ldw=ld, lddx=ld, stream=stream(), **ws.args())
+        assert np.array_equal(fx.double().cpu().numpy(), rounded(r @ w, dt))
+        fx.copy_(torch.from_numpy(x).cuda())
+        dw, db = empty(N, K, "f32"), empty(1, N, "f32")
+        pc.linear_grad_weight(fr, fx, dw, CODE[dt], M, N, K, db=db, lddz=ld, ldx=ld, stream=stream(), **ws.args())
+        assert np.array_equal(dw.get(), r.T @ x) and np.array_equal(db.get()[0], r.sum(0))
+        ws.check()
+
+
 def test_products_run_twice_alike_and_in_place():
     import torch
     rng = np.random.default_rng(15)
