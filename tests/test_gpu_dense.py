@@ -459,6 +459,20 @@ def test_products_of_rows_that_lie_2_to_the_20_elements_apart(dt):
         ws.check()
 
 
+@pytest.mark.parametrize("dt", TYPES)
+def test_few_rows_whose_long_sums_are_shared_are_exact_on_whole_numbers(dt):
+    rng = np.random.default_rng(23)
+    for M, N, K in [(1, 16, 20000), (5, 200, 9001), (16, 1000, 12000), (2, 2001, 8192), (7, 70, 4097)]:
+        say("few rows", dt, M, N, K)
+        assert pc.linear_workspace(CODE[dt], M, N, K) > 0
+        # sums stay below 6 * 20,000 + 80 < 2^24 and, 2 * sqrt(K) each, far inside fp16's range
+        x, w, r, b = whole(rng, (M, K), 3), whole(rng, (N, K), 2), whole(rng, (M, N), 50), whole(rng, N, 30)
+        for place in ((0, 0), (8, 16), (3, 1)):
+            y, z = _linear(x, w, dt, b, r, "relu", True, *place)
+            yy, zz = D.linear(x, w, b, r, "relu", True)
+            assert np.array_equal(z, rounded(zz, dt)) and np.array_equal(y, rounded(yy, dt)), (dt, place, M, N, K)
+
+
 def test_products_run_twice_alike_and_in_place():
     import torch
     rng = np.random.default_rng(15)
