@@ -37,7 +37,7 @@ Plan plan_product(int dtype, int I, int J, int C, bool forward) {
         // 25088 -> 1024, fp16, one row, 64 workgroups 30.1 us, 256 15.1; -> 2000, 125 31.2, 250 23.5.  What is saved has to pay for a second
         // launch and the parts, some 56 stages: 4096 -> 1000, 63 workgroups 7.1 us, 252 7.7; -> 256, 16 rows, 64 8.5, 128 7.6)
         p.tile = kTiles;
-        const long long tiles = (J + 15ll) / 16, most = std::max(1ll, std::min({kComputeUnits / tiles, stages / 8ll, 32ll}));
+        const long long tiles = (J + 15ll) / 16, most = std::max(1ll, std::min({kComputeUnits / tiles, stages / 8ll, 16ll}));
         splits = stages - stages / most >= 56 ? most : 1;
     } else {
         double best = 0;
