@@ -122,7 +122,8 @@ int pconv_layer_norm(const void* x, long long ldx, const float* gamma, const flo
  * The backward pass of layer norm.  With h = (x - mean) * rstd and g = dy * gamma:
  *     dx = rstd * (g - sum(g) / D - h * sum(g * h) / D),  dgamma[d] = sum over rows of dy * h,  dbeta[d] = sum over rows of dy
  *   dy, x         device, dtype[rows][D], row strides lddy, ldx
- *   mean, rstd    device, float[rows], from pconv_layer_norm
+ *   mean, rstd    device, float[rows], from pconv_layer_norm.  (mean is rounded to fp32: h is off by half a unit of mean's last
+ *                 place times rstd, which counts in rows whose spread is small against their level)
  *   gamma         device, float[D], or NULL for ones
  *   dx            device, dtype[rows][D], row stride lddx, or NULL; may be dy or x itself with the same row stride
  *   dgamma, dbeta device, float[D], or NULL (each of its own)

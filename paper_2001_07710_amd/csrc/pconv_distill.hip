@@ -8,10 +8,11 @@
 // with the running maximum and sum of a softmax in the first pass.  The entries are one wave's work, beside the reductions of the
 // others; after the row's w * T * q has been stored the entries' places are stored again with their p taken off, by the first entry of
 // each index (for all that share it).
-// 8192 x 32001, bf16, 64 entries: 219 us, 4.8 TB/s (a copy reaches 5.17).  With the entries in front of the row's loads, and every
-// exponential taken twice, it took 400.  4096 x 128000: 488 us, 4.3 TB/s (4.0 with the row read again; one workgroup fills a compute
-// unit there, and the exponentials are taken twice).  256 x 1000: 6 us, the latency of the entries' and the row's loads and four
-// reductions.  Few rows of many logits are a compute unit's work each: one of 128,000 takes 20 us.
+// 8192 x 32001, bf16, 64 entries: 220 us, 4.8 TB/s (a copy reaches 5.17), 239 with three tensors of logits by turns.  With the entries in
+// front of the row's loads, and every exponential taken twice, it took 400.  4096 x 128000: 484 us, 4.3 TB/s (4.0 with the row read again;
+// one workgroup fills a compute unit there, and the exponentials are taken twice), the gradient alone from kept statistics 424.  256 x 1000:
+// 6 us, the latency of the entries' and the row's loads and four reductions.  Few rows of many logits are a compute unit's work each: one of
+// 128,000 takes 20 us, the gradient alone 13.
 #include "pconv_dense_util.h"
 
 namespace pconv {

@@ -27,6 +27,8 @@ constexpr int kMostSplits = 128;
 
 // Tile and split of a product of I x J results over C: the cheapest by these prices.  A split costs a second launch and its parts, written
 // and read again at about 4.5 TB/s.
+// The prices are those of rows that are aligned to 16 bytes.  Others go through registers, 0.6 us a stage on the smallest tile, and the middle
+// tile stands in for the largest, with the same split: the workspace does not depend on strides.
 Plan plan_product(int dtype, int I, int J, int C, bool forward) {
     Plan p;
     const int stage = kStageBytes / elem_bytes(dtype);
@@ -96,7 +98,8 @@ bool bad_element_alignment(int dtype, const void* p) { return !aligned_to(p, ele
 bool bad_act(int act) { return act < PCONV_ACT_NONE || act > PCONV_ACT_SILU; }
 bool bad_workspace(const void* ws, size_t have, size_t need) { return need && (!ws || have < need || !aligned_to(ws, 16)); }
 
-// ---- column sums of dz (the bias gradient): a workgroup sums a strip of rows for 512 columns, in the order of the rows
+// ---- column sums of dz (the bias gradient): a workgroup sums a strip of rows for 512 columns, in the order of the rows.  8192 x 4096, bf16: 13
+// us, what memory takes for dz.  (Few columns leave most lanes idle, and there are 64 strips at most: 200,000 x 64, bf16, 177 us.)
 constexpr int kSumCols = 512, kMostStrips = 64;
 int sum_strips(int M, int N) {
     const int wide = (N + kSumCols - 1) / kSumCols;
@@ -156,6 +159,8 @@ size_t strip_bytes(int M, int N) {
     return strips > 1 ? ((size_t)strips * N * sizeof(float) + 15) / 16 * 16 : 0;
 }
 
+// dz = dy * act'(z), eight values a thread: memory bounds it.  8192 x 4096, bf16: 37 us with ReLU, 39 with GELU (5.2 to 5.4 TB/s, part of it
+// from the cache behind L2); 64 x 4096: 4.5 us, a launch.
 template <int DT>
 __global__ __launch_bounds__(256) void activation_grad_kernel(const typename Store<DT>::T* dy, long long lddy, const typename Store<DT>::T* z,
                                                               long long ldz, typename Store<DT>::T* dz, long long lddz, int M, int N, int act) {

@@ -19,9 +19,10 @@
 // largest tile; through no window they would be pieces of 8 bytes).
 //
 // What bounds it.  Large products: the chip's power.  With fewer stalls a stage (2,570 clocks of which 2,048 are MFMAs on the largest tile)
-// the clock falls and the time stays: 1.4 to 2 GHz under these loops.  8192 x 4096 -> 16384, bf16: 780 us, 1.41 PFLOP/s, with z kept
-// and GELU 850; the library's plain product there 709.  Gradients of 8192 x 4096 -> 4096: input 220 us (1.25 PFLOP/s), weights 224.  Per
-// tile of 256 x 256 the results take 13,000 clocks, during which nothing is multiplied: a wave has its SIMD's registers to itself.
+// the clock falls and the time stays: 1.4 to 2 GHz under these loops.  8192 x 4096 -> 16384, bf16, medians of calls in a row: 787 us,
+// 1.40 PFLOP/s, with z kept and GELU 838; the library's plain product there 709.  Gradients of 8192 x 4096 -> 4096: input 208 us
+// (1.32 PFLOP/s), with GELU's slope 226, weights 203.  (The means of a kernel trace are 5 to 12 % longer.)  Per tile of 256 x 256 the results
+// take 13,000 clocks, during which nothing is multiplied: a wave has its SIMD's registers to itself.
 // Small products: a launch, the latency of two stages, and the results' way out (512^3: 5.4 us).
 #include <type_traits>
 #include <utility>

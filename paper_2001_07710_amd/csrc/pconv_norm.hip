@@ -8,7 +8,8 @@
 // Workgroups walk over the rows, several short ones at a time, the next ones under way while these are worked on, so that a
 // thread's gamma and beta stay in registers too; in the backward pass so do its columns' sums of dy * h and dy, which meet at the
 // end: the threads with the same columns in LDS, the workgroups in the workspace, one part for a compute unit, added in a second launch.
-// Longer rows (than 1024 threads hold) are read twice or three times, from the caches.
+// Longer rows (than 1024 threads hold) are read twice or three times, from the caches, one workgroup to a row: 2000 x 25088, fp16, 64 us
+// forward, 112 backward in three launches (once through memory: 39 and 58); 64 rows 8 and 15.
 // 16384 x 4096, bf16: forward 48 us (5.5 TB/s, part of it from the cache behind L2), backward 77 us with the column sums (5.2 TB/s; a
 // copy reaches 5.17).  200704 x 64, fp16: forward 15 us (3.4 TB/s), backward 20 (3.9): there a wave's row is one load of its
 // lanes, and the shuffles of eight rows at a time are a third of its instructions.  (Forward without `rest`: 47 and 14.2.)
@@ -444,7 +445,8 @@ __global__ __launch_bounds__(kLong) void norm_grad_long_kernel(const NormArgs p)
     }
 }
 
-// Column sums of dy * h and dy over a strip of rows: a wave's lanes hold eight columns each, its workgroup's four waves take turns.
+// Column sums of dy * h and dy over a strip of rows: a wave's lanes hold eight columns each, its workgroup's four waves take turns.  (Four
+// rows ahead in 16 bits take all 256 registers, one wave a SIMD: 2000 x 25088, fp16, 37 us, what memory takes.)
 constexpr int kSumCols = 512;
 template <int DT>
 __global__ __launch_bounds__(256) void norm_columns_kernel(const NormArgs p, int per) {
@@ -550,7 +552,8 @@ Spread spread(int pieces) {
     return {0, 0, 1};
 }
 #define PCONV_SPREADS(X) X(8, 1, 4) X(16, 1, 4) X(32, 1, 4) X(64, 1, 4) X(64, 2, 2) X(256, 1, 2) X(256, 2, 1) X(512, 2, 1) X(1024, 2, 1)
-// (the backward pass needs three times the registers)
+// (the backward pass needs three times the registers; 1024 threads with two pieces of 16 bits have 128 each, and 68 bytes a lane do not fit:
+// 4096 x 16384, bf16, 97 us, where memory takes 78)
 Spread grad_spread(int pieces) {
     if (pieces <= 8) return {8, 1, 2};
     if (pieces <= 16) return {16, 1, 2};
