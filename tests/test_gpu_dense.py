@@ -1097,3 +1097,89 @@ def test_offsets_that_pass_32_bits():
     torch.cuda.synchronize()
     want = x[rows - 5:].double().sum(0)
     assert bool(((dw.double() - want).abs() <= 8 * U32 * x[rows - 5:].double().abs().sum(0)).all())
+
+
+@pytest.mark.parametrize("dt", TYPES)
+def test_in_place_in_every_path(dt):
+    """A residual that is y, an added gradient that is dx, a norm's y that is x, its dx that is x or dy: the bits of the call beside them."""
+    import torch
+    rng = np.random.default_rng(44)
+    real = lambda *shape: torch.from_numpy(rng.standard_normal(shape)).cuda().to(ttype(dt))  # noqa: E731
+    for M, N, K, pad in [(3, 70, 5000, 0), (150, 140, 203, 0), (100, 130, 5000, 0), (1030, 1100, 136, 0), (2100, 2200, 264, 5), (4600, 6143, 72, 0)]:
+        say("in place", dt, M, N, K, pad)
+        x, w, r = real(M, K + pad), real(N, K + pad), real(M, N)
+        ws = Scratch(max(pc.linear_workspace(CODE[dt], M, N, K), pc.linear_grad_input_workspace(CODE[dt], M, N, K)))
+        for flags in (0, pc.FLAG_RESIDUAL_FIRST):
+            y, z, one = r.clone(), torch.empty_like(r), torch.empty_like(r)
+            for out in (one, y):
+                pc.linear(x, w, out, CODE[dt], M, N, K, residual=r if out is one else y, z=z, act=pc.ACT_SILU, flags=flags, ldx=K + pad,
+                          ldw=K + pad, stream=stream(), **ws.args())
+            assert torch.equal(y, one), (dt, M, N, K, flags)
+        add = real(M, K)
+        dx, one = add.clone(), torch.empty_like(add)
+        for out in (one, dx):
+            pc.linear_grad_input(r, w, out, CODE[dt], M, N, K, z=x, act=pc.ACT_SILU, add=add if out is one else dx, ldw=K + pad, ldz=K + pad,
+                                 stream=stream(), **ws.args())
+        assert torch.equal(dx, one), (dt, M, N, K)
+    for Dn in (33, 100, 200, 500, 1000, 2000, 4001, 8000, 16001, 33000):
+        rows = max(7, 2000000 // Dn // 8)
+        say("norm in place", dt, rows, Dn)
+        x, dy, gamma = real(rows, Dn), real(rows, Dn), vec(rng.standard_normal(Dn))
+        mean, rstd = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+        one, same = torch.empty_like(x), x.clone()
+        for a, b in ((x, one), (same, same)):
+            pc.layer_norm(a, b, CODE[dt], rows, Dn, gamma=gamma, beta=gamma, mean=mean, rstd=rstd, stream=stream())
+        assert torch.equal(one, same), (dt, rows, Dn)
+        need, got = pc.layer_norm_grad_workspace(CODE[dt], rows, Dn), []
+        for which in range(3):
+            a, g = x.clone(), dy.clone()
+            out = (torch.empty_like(x), a, g)[which]
+            sums, ws = torch.empty(2, Dn, device="cuda"), Scratch(need)
+            pc.layer_norm_grad(g, a, out, mean, rstd, CODE[dt], rows, Dn, gamma=gamma, dgamma=sums[0], dbeta=sums[1], stream=stream(), **ws.args())
+            got.append((out, sums))
+        assert all(torch.equal(o, got[0][0]) and torch.equal(s, got[0][1]) for o, s in got[1:]), (dt, rows, Dn)
+
+
+def test_as_many_rows_as_there_may_be():
+    """2^30 rows of products and 2^31 - 1 of a norm, a block of rows over and over: every copy of it gives what the block alone gives."""
+    import torch
+    rng = np.random.default_rng(43)
+    copies, rows, K, N = 1 << 10, 1 << 20, 8, 16
+    M = copies * rows
+    block, w = (torch.from_numpy(whole(rng, s, 3)).cuda().bfloat16() for s in ((rows, K), (N, K)))
+    x = torch.empty((copies, rows, K), dtype=torch.bfloat16, device="cuda")
+    x.copy_(block)
+    y = torch.empty((copies, rows, N), dtype=torch.bfloat16, device="cuda")
+    assert pc.linear_workspace(pc.BF16, M, N, K) == 0 and pc.linear_grad_input_workspace(pc.BF16, M, N, K) == 0
+    say("linear", M)
+    pc.linear(x, w, y, pc.BF16, M, N, K, act=pc.ACT_RELU, stream=stream())
+    torch.cuda.synchronize()
+    want = (block.float() @ w.float().t()).clamp(min=0).bfloat16()           # (whole numbers below 72)
+    assert bool((y[0] == want).all()) and all(bool((y[at:at + 64] == y[0]).all()) for at in range(0, copies, 64))
+    say("linear_grad_input", M)
+    pc.linear_grad_input(y, w, x, pc.BF16, M, N, K, stream=stream())
+    torch.cuda.synchronize()
+    want = (want.float() @ w.float()).bfloat16()
+    assert bool((x[0] == want).all()) and all(bool((x[at:at + 64] == x[0]).all()) for at in range(0, copies, 64))
+    y[:-1] = 0                                                               # the last block's rows alone
+    y[-1, :-9] = 0
+    x.copy_(block)
+    dw = torch.full((N, K), 55.0, device="cuda")
+    ws = Scratch(pc.linear_grad_weight_workspace(pc.BF16, M, N, K))
+    say("linear_grad_weight", M)
+    pc.linear_grad_weight(y, x, dw, pc.BF16, M, N, K, stream=stream(), **ws.args())
+    torch.cuda.synchronize()
+    ws.check()
+    assert bool((dw.double() == y[-1, -9:].double().t() @ block[-9:].double()).all())
+    del x, y
+    M, D_ = (1 << 31) - 1, 2
+    x = torch.empty((1 << 31, D_), dtype=torch.bfloat16, device="cuda")
+    x.view(1 << 10, 1 << 21, D_).copy_(torch.randn((1 << 21, D_), device="cuda"))
+    small, last = torch.empty((1 << 21, D_), dtype=torch.bfloat16, device="cuda"), x[-1].clone()
+    pc.layer_norm(x, small, pc.BF16, 1 << 21, D_, stream=stream())
+    say("layer_norm", M)
+    pc.layer_norm(x, x, pc.BF16, M, D_, stream=stream())
+    torch.cuda.synchronize()
+    assert bool((x[-1] == last).all())
+    x[-1] = small[-1]
+    assert all(bool((x.view(1 << 10, 1 << 21, D_)[at:at + 64] == small).all()) for at in range(0, 1 << 10, 64))
