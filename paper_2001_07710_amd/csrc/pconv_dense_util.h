@@ -131,7 +131,8 @@ __device__ __forceinline__ float bounded(float z) { return __builtin_amdgcn_fmed
 constexpr float kLog2E = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
 // An exponent in two parts, `low` being what the first one's rounding left.  WIDE (fp32): rounded as one number an exponent x costs 2^x some
 // |x| units, up to a hundred in the tails; with the rest put right behind the exponential that is one.  Otherwise `low` is 0: a hundred
-// units are nothing that 16 bits keep.
+// units are nothing that 16 bits keep.  (fp32, 4096 x 64 -> 4096: SiLU 38 -> 40 us, GELU's tanh form 38 -> 44, GELU 48 -> 54; 2048 x 512 ->
+// 2048 40.3 -> 40.7, 40.3 -> 42, 43 -> 45.)
 struct Exponent {
     float x, low;
 };
